@@ -411,6 +411,9 @@ def run(state):
         return _plain_rope(c, st["x"], st["pos"], st["out"])
     if c["kind"] == "append":
         if own:
+            if c["n"] > c["T"]:
+                # an earlier pass took the unfinished block's 16-bit rows further: given again
+                st["layer"].append(st["k0"], st["v0"], st["start"], n_new=st["pos"] - st["start"])
             st["layer"].append(st["k"], st["v"], st["pos"], n_new=st["n_new"])
             st["layer"].read(st["end"], st["start"], st["k_out"], st["v_out"])
             return st["k_out"], st["v_out"]
