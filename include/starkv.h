@@ -361,6 +361,220 @@ int32_t       starkv_decode_fast_blocks(const starkv_plan* plan, int32_t max_ctx
 starkv_status starkv_read_stream(const void* src, size_t bytes, int32_t workgroups, void* sink,
                                  size_t sink_bytes, starkv_stream_t stream);
 
+/* ==============================================================================
+ * Uncompressed layers.  The method leaves some layers of a model uncompressed
+ * (App. A.3).  The entry points below serve such a layer: rotary positions, a
+ * cache of keys and values in 8 bits, attention over it, and eviction of the
+ * blocks that gathered the least attention.  The conventions at the top hold.
+ * ============================================================================== */
+
+/* Element strides of a [B][n][H][d] array; channels are contiguous.  NULL where a
+ * call takes one: packed ([B][n][H][d] without gaps).  Inputs may have any strides
+ * (0 repeats a row); an output's rows must not overlap: the stride of a dimension
+ * longer than one is at least d (INVALID_ARG). */
+typedef struct { int64_t batch, token, head; } starkv_strides;
+
+/* ------------------------------------------------------------------------------
+ * Rotary positions.  Of the d channels of a head the first R = rotary_dim are
+ * rotated in pairs j = 0..R/2-1, by the angle a_j = position * f_j:
+ *   y_p = m (x_p cos a_j - x_q sin a_j),  y_q = m (x_q cos a_j + x_p sin a_j)
+ *   HALF:        (p, q) = (j, j + R/2)   (the pairing of starkv_decode_attn's keys)
+ *   INTERLEAVED: (p, q) = (2j, 2j + 1)
+ * and the others are copied.  With f = theta^(-2j/R), s = factor, L0 = original_ctx and
+ * n_j = L0 f / 2 pi (turns over the original context):
+ *   PLAIN   f_j = f
+ *   LINEAR  f_j = f / s                                  (positions interpolated)
+ *   NTK     f_j = (theta s^(R/(R-2)))^(-2j/R)            (base raised; R > 2)
+ *   BANDS   f_j = f (w + (1 - w)/s),  w = (n_j - turns_low)/(turns_high - turns_low)
+ *           clamped to [0, 1]: pairs with many turns keep their frequency
+ *   YARN    f_j = f (1 - r) + (f/s) r,  r = (j - j0)/(j1 - j0) clamped to [0, 1], where
+ *           j0 = max(floor(J(turns_high)), 0), j1 = min(ceil(J(turns_low)), R - 1),
+ *           J(n) = R ln(L0/(2 pi n)) / (2 ln theta), and j1 - j0 is at least 0.001
+ * m = gain; gain = 0 means 1, and 0.1 ln s + 1 for YARN.  Frequencies and angles are
+ * taken in fp64 and reduced to a turn before they are rounded. */
+typedef enum { STARKV_ROPE_HALF = 0, STARKV_ROPE_INTERLEAVED = 1 } starkv_rope_layout;
+typedef enum { STARKV_ROPE_PLAIN = 0, STARKV_ROPE_LINEAR = 1, STARKV_ROPE_NTK = 2,
+               STARKV_ROPE_BANDS = 3, STARKV_ROPE_YARN = 4 } starkv_rope_scaling;
+
+typedef struct {
+  int32_t head_dim;      /* d: even, 2..512 */
+  int32_t rotary_dim;    /* R: even, 2..d */
+  int32_t layout;        /* starkv_rope_layout */
+  int32_t scaling;       /* starkv_rope_scaling */
+  double  theta;         /* base, > 1 */
+  double  factor;        /* s >= 1 (all but PLAIN) */
+  int32_t original_ctx;  /* L0 >= 1 (BANDS, YARN) */
+  double  turns_low, turns_high;  /* 0 < low < high (BANDS, YARN); both 0: 1 and 4 for
+                                     BANDS, 1 and 32 for YARN */
+  double  gain;          /* m > 0, or 0 for the default */
+  int32_t dtype;         /* starkv_dtype of x and out: F16, BF16 or F32 */
+} starkv_rope_config;
+
+typedef struct starkv_rope_plan starkv_rope_plan;   /* opaque, immutable */
+
+starkv_status starkv_rope_plan_create(const starkv_rope_config* cfg, starkv_rope_plan** out);
+void          starkv_rope_plan_destroy(starkv_rope_plan* plan);
+
+/* starkv_rope -- rotates n_heads heads of batch x n_tokens tokens.
+ *   x, out       device [B][n][H][d] in the plan's dtype, aligned to an element (16-byte
+ *                aligned rows are read and written in wide accesses).  out may be x with
+ *                the same strides; otherwise the two must not overlap.
+ *   positions    device int32 [B][n], any value.
+ *   inverse      nonzero: the transposed map (angles negated, the same gain), which is the
+ *                gradient with respect to x.
+ * Errors: INVALID_ARG, UNSUPPORTED (sizes beyond the grid), ALIGNMENT, HIP. */
+starkv_status starkv_rope(const starkv_rope_plan* plan, const void* x, const starkv_strides* xs,
+                          void* out, const starkv_strides* os, const int32_t* positions,
+                          int32_t batch, int32_t n_tokens, int32_t n_heads, int32_t inverse,
+                          starkv_stream_t stream);
+
+/* ------------------------------------------------------------------------------
+ * Cache of keys and values in 8 bits, with one fp32 scale for each block of T =
+ * block_tokens tokens of a KV head, for keys and for values.  Token t lies in block t/T.
+ * A block is stored in 8 bits when its last token is appended, straight from the 16-bit
+ * rows: every value is rounded once, however the tokens arrived.  The rows of an
+ * unfinished block stay in 16 bits; they are kept for the last two blocks, so that
+ * tokens can be taken back (see starkv_dense_append).
+ *   scale s = absmax / M in fp32 (round to nearest), M = 127 (INT8) or 448 (E4M3, the OCP
+ *   8-bit float with 4 exponent and 3 mantissa bits); code = round-to-nearest-even(x / s),
+ *   decided exactly; the cached value is code * s.  A block of zeros has s = 0.  A block with a
+ *   NaN or an infinity has s = NaN and codes 0: what attends to it is NaN.
+ * Planes, each starting on a 256-byte boundary:
+ *   codes   n_blocks blocks of 2 T d bytes: T/16 key subtiles, then T/16 value subtiles, of
+ *           16 tokens each (16 d bytes).  In a subtile, with 64-channel groups i:
+ *           keys    token tau, channel i*64 + 16*a + c at i*1024 + a*256 + tau*16 + c
+ *           values  token 4*a + r, channel i*64 + 16*j + c at i*1024 + a*256 + c*16 + 4*j + r
+ *           INT8 bytes hold code + 128.
+ *   scales  n_blocks pairs (keys, values) of fp32
+ *   tails   16-bit rows of the last two blocks, per sequence and KV head: 2T key rows
+ *           [2T][d], then values [2T/16][d][16]; token t is row t % 2T
+ * Block j of KV head g of sequence b is pool block block_table[(b*H_kv + g)*J + j], J =
+ * ceil(capacity / T).  Sequences may share finished blocks by naming the same pool block. */
+typedef enum { STARKV_CODE_INT8 = 0, STARKV_CODE_E4M3 = 1 } starkv_code;
+
+typedef struct {
+  int32_t batch;          /* sequences B, <= 32767 */
+  int32_t n_q_heads;      /* H_q <= 64, a multiple of n_kv_heads; query head i reads KV head
+                             floor(i*H_kv/H_q) */
+  int32_t n_kv_heads;     /* H_kv <= 16 */
+  int32_t head_dim;       /* d: 64 or 128 */
+  int32_t capacity;       /* tokens per sequence, 1..524288 */
+  int32_t code;           /* starkv_code */
+  int32_t block_tokens;   /* T: 16, 32, 64 or 128 */
+  int32_t dtype;          /* starkv_dtype of keys, values, queries and outputs: F16 or BF16 */
+  int32_t n_blocks;       /* blocks in the pool, n_blocks * T < 2^31 */
+  double  softmax_scale;  /* > 0, or 0 for 1/sqrt(d) */
+  /* device int32 [B][H_kv][J], 4-byte aligned.  The pointer is fixed at plan creation, the
+   * contents are read by every call at its place in the stream, and starkv_dense_evict may
+   * rewrite them.  Append drops blocks whose entry is outside [0, n_blocks); the other
+   * calls clamp such entries into the pool and read whatever is there. */
+  int32_t* block_table;
+} starkv_dense_config;
+
+typedef struct {
+  int64_t total_bytes;
+  int64_t code_offset, scale_offset, tail_offset;
+  int64_t block_bytes;            /* 2 T d */
+  int64_t tail_bytes;             /* of one sequence and KV head */
+  int32_t blocks_per_head;        /* J */
+} starkv_dense_layout;
+
+typedef struct starkv_dense_plan starkv_dense_plan;   /* opaque, immutable */
+
+/* Errors: INVALID_ARG, UNSUPPORTED, ALIGNMENT. */
+starkv_status starkv_dense_plan_create(const starkv_dense_config* cfg, starkv_dense_plan** out);
+void          starkv_dense_plan_destroy(starkv_dense_plan* plan);
+size_t        starkv_dense_cache_bytes(const starkv_dense_plan* plan);
+starkv_status starkv_dense_cache_layout(const starkv_dense_plan* plan, starkv_dense_layout* out);
+
+/* starkv_dense_append -- writes up to n_new new tokens of every sequence.
+ *   cache        device, starkv_dense_cache_bytes(plan) bytes, 256-byte aligned (any contents).
+ *   k, v         device [B][n_new][H_kv][d] in the plan's dtype, 2-byte aligned; keys already
+ *                rotated (starkv_rope).
+ *   pos_dev      device int32 [B]: position of the first new token.  Tokens are appended
+ *                without gaps: the cache holds the tokens before pos[b].  A position before
+ *                the sequence's end takes tokens back.  The 16-bit rows of a token stay until a
+ *                token two blocks further on is appended: pos[b] may be any multiple of T, and
+ *                any position whose block, or the next, holds the furthest token appended so far
+ *                (so up to T tokens can always be taken back).
+ *   n_new_dev    device int32 [B]: new tokens of each sequence, clamped to [0, n_new]; NULL:
+ *                n_new in all.
+ * Tokens outside [0, capacity) are dropped.  The caller advances its lengths.
+ * Errors: INVALID_ARG, ALIGNMENT, HIP. */
+starkv_status starkv_dense_append(const starkv_dense_plan* plan, void* cache, const void* k,
+                                  const starkv_strides* ks, const void* v,
+                                  const starkv_strides* vs, const int32_t* pos_dev,
+                                  int32_t n_new, const int32_t* n_new_dev,
+                                  starkv_stream_t stream);
+
+/* starkv_dense_read -- rows start[b] .. start[b]+n-1 of every sequence and KV head as the
+ * cache holds them: code * s in finished blocks, the 16-bit rows of the unfinished one.
+ *   ctx_len_dev  device int32 [B]: tokens in the cache (clamped to [0, capacity]); rows outside
+ *                [0, ctx_len[b]) are zero.
+ *   k_out, v_out device [B][n][H_kv][d] in out_dtype (F16, BF16 or F32), aligned to an element;
+ *                either may be NULL.
+ * Errors: INVALID_ARG, ALIGNMENT, HIP. */
+starkv_status starkv_dense_read(const starkv_dense_plan* plan, const void* cache,
+                                const int32_t* ctx_len_dev, const int32_t* start_dev, int32_t n,
+                                void* k_out, const starkv_strides* ks, void* v_out,
+                                const starkv_strides* vs, int32_t out_dtype,
+                                starkv_stream_t stream);
+
+/* Bytes of workspace for starkv_dense_attn with up to n_q query tokens per sequence and
+ * contexts up to max_ctx; with_weights nonzero: also for calls that gather weights. */
+size_t        starkv_dense_workspace_bytes(const starkv_dense_plan* plan, int32_t n_q,
+                                           int32_t max_ctx, int32_t with_weights);
+
+/* starkv_dense_attn -- attention of the last query tokens of every sequence over its cache.
+ *   q            device [B][n_q][H_q][d] in the plan's dtype, 2-byte aligned, rotated.
+ *   n_q          query tokens per sequence, >= 1: one for a decode step, more for drafted
+ *                tokens or a prompt's chunk, whose keys and values are appended before.
+ *   q_len_dev    device int32 [B]: query tokens of each sequence, clamped to [0, n_q]; NULL:
+ *                n_q in all.  Rows of out at or past q_len[b] are left as they were.
+ *   ctx_len_dev  device int32 [B]: tokens in the cache, clamped to [0, max_ctx].  Query token j
+ *                is token ctx_len[b] - q_len[b] + j and attends to the tokens up to itself;
+ *                where there is none (a negative position) its output is zero.
+ *   max_ctx      host upper bound of ctx_len, 1 <= max_ctx <= capacity.
+ *   out          device [B][n_q][H_q][d] in the plan's dtype, 2-byte aligned.
+ *   weights      device float [B][H_kv][J], or NULL.  Block j of KV head g gains the
+ *                probabilities of its tokens, summed over the query tokens and the query heads
+ *                of g, in a fixed order (the unfinished block among them).  Needs
+ *                n_q * H_q/H_kv <= 64 (UNSUPPORTED).
+ *   ws           device, starkv_dense_workspace_bytes(plan, n_q, max_ctx, weights != NULL)
+ *                bytes, 256-byte aligned.
+ * Scores, softmax sums and accumulators are fp32; probabilities enter the product with the
+ * values in fp16 (with two bf16 parts for the unfinished block of a BF16 plan).
+ * Errors: INVALID_ARG, UNSUPPORTED, CAPACITY, WORKSPACE, ALIGNMENT, HIP. */
+starkv_status starkv_dense_attn(const starkv_dense_plan* plan, const void* cache, const void* q,
+                                const starkv_strides* qs, int32_t n_q, const int32_t* q_len_dev,
+                                const int32_t* ctx_len_dev, int32_t max_ctx, void* out,
+                                const starkv_strides* os, float* weights, void* ws,
+                                size_t ws_bytes, starkv_stream_t stream);
+
+/* starkv_dense_evict -- shortens every sequence to about `keep` finished blocks per KV head.
+ * Of n = ctx_len[b]/T finished blocks the first `sink`, the last `recent` and those of the
+ * others with the largest weights stay (of equal ones the first; a NaN counts as the largest).
+ * n' = n - 2*floor((n - keep)/2) stay, i.e. keep or keep + 1, if n > keep; an even number
+ * leaves because the 16-bit rows of the unfinished block lie by the parity of its number.
+ * Blocks are evicted whole: only the block table is rewritten and nothing is requantized.
+ *   weights      device float [B][H_kv][J], as starkv_dense_attn gathers them.
+ *   ctx_len_dev  device int32 [B], clamped to [0, capacity].
+ *   keep >= 1; sink, recent >= 0; sink + recent <= keep.
+ *   table_out    device int32 [B][H_kv][J]: the kept blocks in their order, then those that
+ *                left in theirs (free for the sequence's next tokens), then entries n.. of the
+ *                table.  NULL: the plan's table, in place.
+ *   weights_out  device float [B][H_kv][J]: the kept blocks' weights, that of the unfinished
+ *                block as entry n', then zeros.  NULL: weights, in place.
+ *   ctx_out      device int32 [B]: ctx_len - (n - n') T.  May be ctx_len_dev (or NULL, the same).
+ * Outputs that are not in place must not overlap inputs.  Positions of later tokens (for
+ * starkv_rope) count on from the unshortened sequence; lengths, and positions of
+ * starkv_dense_append, from ctx_out.
+ * Errors: INVALID_ARG, ALIGNMENT, HIP. */
+starkv_status starkv_dense_evict(const starkv_dense_plan* plan, float* weights,
+                                 int32_t* ctx_len_dev, int32_t keep, int32_t sink,
+                                 int32_t recent, int32_t* table_out, float* weights_out,
+                                 int32_t* ctx_out, starkv_stream_t stream);
+
 const char*   starkv_status_string(starkv_status status);
 const char*   starkv_last_error(void);          /* thread-local, never NULL */
 

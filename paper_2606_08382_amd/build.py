@@ -24,7 +24,9 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
 
 UNITS = [(f, [f"-DSK_D={d}", f"-DSK_QM={q}"]) for f in ("split_poly.hip", "decode.hip")
           for d in (128, 64) for q in (2, 3, 1, 0)]
-UNITS += [("starkv_host.cpp", []), ("append.hip", []), ("output.hip", []), ("stream.hip", []),
+UNITS += [("dense_attn.hip", [])]
+UNITS += [("starkv_host.cpp", []), ("dense_host.cpp", []), ("rope.hip", []),
+          ("dense_cache.hip", []), ("append.hip", []), ("output.hip", []), ("stream.hip", []),
           ("decode.hip", ["-DSK_COMMON"]), ("split_poly.hip", [])]
 
 

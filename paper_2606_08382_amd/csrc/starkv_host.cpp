@@ -11,6 +11,7 @@
 #include <string>
 
 #include "starkv.h"
+#include "dense.h"
 #include "starkv_internal.h"
 
 using namespace starkv;
@@ -61,6 +62,21 @@ constexpr int kMaxSplitTokens = 8192;   // tokens per split (bounds the RoPE rot
 constexpr int kMaxCtx = 64 * kMaxSplitTokens;   // longest context (524288 tokens)
 
 }  // namespace
+
+namespace starkv {
+
+// The same for the library's other host files.
+starkv_status fail_with(starkv_status st, const char* fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof(buf), fmt, ap);
+  va_end(ap);
+  g_last_error = buf;
+  return st;
+}
+
+}  // namespace starkv
 
 // The polynomial-rotation split kernel for a plan's heads (ok: whether it applies).
 struct PolyPlan {

@@ -20,6 +20,9 @@ STATUS_NAMES = {0: "OK", 1: "INVALID_ARG", 2: "UNSUPPORTED", 3: "CAPACITY", 4: "
 Q_F16, Q_INT4, Q_MIX8_4, Q_MIX4_3 = 0, 1, 2, 3
 DT_F16, DT_BF16, DT_F32 = 0, 1, 2   # F32: attention output only
 MAX_KV_HEADS = 16
+CODE_INT8, CODE_E4M3 = 0, 1
+ROPE_HALF, ROPE_INTERLEAVED = 0, 1
+ROPE_PLAIN, ROPE_LINEAR, ROPE_NTK, ROPE_BANDS, ROPE_YARN = 0, 1, 2, 3, 4
 
 
 class StarkvError(RuntimeError):
@@ -59,6 +62,32 @@ class starkv_decode_info(C.Structure):
                 ("split_tokens", C.c_int32), ("lds_bytes", C.c_int32)]
 
 
+class starkv_strides(C.Structure):
+    """Element strides of a [B][n][H][d] array."""
+    _fields_ = [("batch", C.c_int64), ("token", C.c_int64), ("head", C.c_int64)]
+
+
+class starkv_rope_config(C.Structure):
+    _fields_ = [("head_dim", C.c_int32), ("rotary_dim", C.c_int32), ("layout", C.c_int32),
+                ("scaling", C.c_int32), ("theta", C.c_double), ("factor", C.c_double),
+                ("original_ctx", C.c_int32), ("turns_low", C.c_double),
+                ("turns_high", C.c_double), ("gain", C.c_double), ("dtype", C.c_int32)]
+
+
+class starkv_dense_config(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("capacity", C.c_int32), ("code", C.c_int32),
+                ("block_tokens", C.c_int32), ("dtype", C.c_int32), ("n_blocks", C.c_int32),
+                ("softmax_scale", C.c_double), ("block_table", C.c_void_p)]
+
+
+class starkv_dense_layout(C.Structure):
+    _fields_ = [("total_bytes", C.c_int64), ("code_offset", C.c_int64),
+                ("scale_offset", C.c_int64), ("tail_offset", C.c_int64),
+                ("block_bytes", C.c_int64), ("tail_bytes", C.c_int64),
+                ("blocks_per_head", C.c_int32)]
+
+
 EXPORTS = ["starkv_plan_create", "starkv_plan_destroy", "starkv_cache_bytes",
            "starkv_cache_layout", "starkv_append_workspace_bytes",
            "starkv_decode_workspace_bytes", "starkv_append", "starkv_decode_attn",
@@ -66,7 +95,11 @@ EXPORTS = ["starkv_plan_create", "starkv_plan_destroy", "starkv_cache_bytes",
            "starkv_decode_split_tokens", "starkv_status_string", "starkv_last_error",
            "starkv_decode_attn_absorbed", "starkv_decode_combine_absorbed",
            "starkv_decode_describe", "starkv_decode_fast_blocks", "starkv_decode_attn_noalloc",
-           "starkv_read_stream"]
+           "starkv_read_stream", "starkv_rope_plan_create", "starkv_rope_plan_destroy",
+           "starkv_rope", "starkv_dense_plan_create", "starkv_dense_plan_destroy",
+           "starkv_dense_cache_bytes", "starkv_dense_cache_layout", "starkv_dense_append",
+           "starkv_dense_read", "starkv_dense_workspace_bytes", "starkv_dense_attn",
+           "starkv_dense_evict"]
 
 _lib = None
 
@@ -117,6 +150,31 @@ def lib():
         L.starkv_decode_fast_blocks.restype = C.c_int32
         L.starkv_read_stream.argtypes = [P, S, C.c_int32, P, S, P]
         L.starkv_read_stream.restype = C.c_int
+        I, ST = C.c_int32, C.POINTER(starkv_strides)
+        L.starkv_rope_plan_create.argtypes = [C.POINTER(starkv_rope_config), C.POINTER(P)]
+        L.starkv_rope_plan_create.restype = C.c_int
+        L.starkv_rope_plan_destroy.argtypes = [P]
+        L.starkv_rope_plan_destroy.restype = None
+        L.starkv_rope.argtypes = [P, P, ST, P, ST, P, I, I, I, I, P]
+        L.starkv_rope.restype = C.c_int
+        L.starkv_dense_plan_create.argtypes = [C.POINTER(starkv_dense_config), C.POINTER(P)]
+        L.starkv_dense_plan_create.restype = C.c_int
+        L.starkv_dense_plan_destroy.argtypes = [P]
+        L.starkv_dense_plan_destroy.restype = None
+        L.starkv_dense_cache_bytes.argtypes = [P]
+        L.starkv_dense_cache_bytes.restype = S
+        L.starkv_dense_cache_layout.argtypes = [P, C.POINTER(starkv_dense_layout)]
+        L.starkv_dense_cache_layout.restype = C.c_int
+        L.starkv_dense_append.argtypes = [P, P, P, ST, P, ST, P, I, P, P]
+        L.starkv_dense_append.restype = C.c_int
+        L.starkv_dense_read.argtypes = [P, P, P, P, I, P, ST, P, ST, I, P]
+        L.starkv_dense_read.restype = C.c_int
+        L.starkv_dense_workspace_bytes.argtypes = [P, I, I, I]
+        L.starkv_dense_workspace_bytes.restype = S
+        L.starkv_dense_attn.argtypes = [P, P, P, ST, I, P, P, I, P, ST, P, P, S, P]
+        L.starkv_dense_attn.restype = C.c_int
+        L.starkv_dense_evict.argtypes = [P, P, P, I, I, I, P, P, P, P]
+        L.starkv_dense_evict.restype = C.c_int
         L.starkv_status_string.argtypes = [C.c_int]
         L.starkv_status_string.restype = C.c_char_p
         L.starkv_last_error.argtypes = []
@@ -312,6 +370,112 @@ def starkv_decode_combine_absorbed(plan: Plan, cache, q, B_k, W_abs, d_out: int,
                                                 _ptr(out), _ptr(ws),
                                                 _nbytes(ws) if ws_bytes is None else ws_bytes,
                                                 _stream(stream)))
+
+
+class RopePlan:
+    """Owns a starkv_rope_plan*; destroyed with the object."""
+
+    def __init__(self, handle: int, cfg: starkv_rope_config):
+        self.handle, self.cfg = handle, cfg
+
+    def __del__(self):
+        if getattr(self, "handle", None) and _lib is not None:
+            _lib.starkv_rope_plan_destroy(self.handle)
+            self.handle = None
+
+
+class DensePlan:
+    """Owns a starkv_dense_plan*; destroyed with the object."""
+
+    def __init__(self, handle: int, cfg: starkv_dense_config):
+        self.handle, self.cfg = handle, cfg
+
+    def __del__(self):
+        if getattr(self, "handle", None) and _lib is not None:
+            _lib.starkv_dense_plan_destroy(self.handle)
+            self.handle = None
+
+
+def make_rope_config(head_dim, theta, rotary_dim=None, layout=ROPE_HALF, scaling=ROPE_PLAIN,
+                     factor=1.0, original_ctx=0, turns_low=0.0, turns_high=0.0, gain=0.0,
+                     dtype=DT_BF16) -> starkv_rope_config:
+    return starkv_rope_config(head_dim, head_dim if rotary_dim is None else rotary_dim, layout,
+                              scaling, float(theta), float(factor), original_ctx,
+                              float(turns_low), float(turns_high), float(gain), dtype)
+
+
+def starkv_rope_plan_create(cfg: starkv_rope_config) -> RopePlan:
+    h = C.c_void_p()
+    _check(lib().starkv_rope_plan_create(C.byref(cfg), C.byref(h)))
+    return RopePlan(h.value, cfg)
+
+
+def starkv_rope(plan: RopePlan, x, xs: Optional[starkv_strides], out,
+                os_: Optional[starkv_strides], positions, batch: int, n_tokens: int,
+                n_heads: int, inverse: int = 0, stream=None) -> None:
+    _check(lib().starkv_rope(plan.handle, _ptr(x), xs, _ptr(out), os_, _ptr(positions), batch,
+                             n_tokens, n_heads, inverse, _stream(stream)))
+
+
+def make_dense_config(batch, n_q_heads, n_kv_heads, head_dim, capacity, n_blocks, block_table,
+                      code=CODE_INT8, block_tokens=64, dtype=DT_BF16,
+                      softmax_scale=0.0) -> starkv_dense_config:
+    """block_table: device int32 [batch][n_kv_heads][ceil(capacity / block_tokens)] (tensor or
+    address)."""
+    return starkv_dense_config(batch, n_q_heads, n_kv_heads, head_dim, capacity, code,
+                               block_tokens, dtype, n_blocks, float(softmax_scale),
+                               _ptr(block_table))
+
+
+def starkv_dense_plan_create(cfg: starkv_dense_config) -> DensePlan:
+    h = C.c_void_p()
+    _check(lib().starkv_dense_plan_create(C.byref(cfg), C.byref(h)))
+    return DensePlan(h.value, cfg)
+
+
+def starkv_dense_cache_bytes(plan: DensePlan) -> int:
+    return lib().starkv_dense_cache_bytes(plan.handle)
+
+
+def starkv_dense_cache_layout(plan: DensePlan) -> starkv_dense_layout:
+    out = starkv_dense_layout()
+    _check(lib().starkv_dense_cache_layout(plan.handle, C.byref(out)))
+    return out
+
+
+def starkv_dense_append(plan: DensePlan, cache, k, ks: Optional[starkv_strides], v,
+                        vs: Optional[starkv_strides], pos, n_new: int, n_new_dev=None,
+                        stream=None) -> None:
+    _check(lib().starkv_dense_append(plan.handle, _ptr(cache), _ptr(k), ks, _ptr(v), vs,
+                                     _ptr(pos), n_new, _ptr(n_new_dev), _stream(stream)))
+
+
+def starkv_dense_read(plan: DensePlan, cache, ctx_len, start, n: int, k_out,
+                      ks: Optional[starkv_strides], v_out, vs: Optional[starkv_strides],
+                      out_dtype: int, stream=None) -> None:
+    _check(lib().starkv_dense_read(plan.handle, _ptr(cache), _ptr(ctx_len), _ptr(start), n,
+                                   _ptr(k_out), ks, _ptr(v_out), vs, out_dtype, _stream(stream)))
+
+
+def starkv_dense_workspace_bytes(plan: DensePlan, n_q: int, max_ctx: int,
+                                 with_weights: bool = False) -> int:
+    return lib().starkv_dense_workspace_bytes(plan.handle, n_q, max_ctx, int(with_weights))
+
+
+def starkv_dense_attn(plan: DensePlan, cache, q, qs: Optional[starkv_strides], n_q: int, q_len,
+                      ctx_len, max_ctx: int, out, os_: Optional[starkv_strides], weights, ws,
+                      ws_bytes: Optional[int] = None, stream=None) -> None:
+    _check(lib().starkv_dense_attn(plan.handle, _ptr(cache), _ptr(q), qs, n_q, _ptr(q_len),
+                                   _ptr(ctx_len), max_ctx, _ptr(out), os_, _ptr(weights),
+                                   _ptr(ws), _nbytes(ws) if ws_bytes is None else ws_bytes,
+                                   _stream(stream)))
+
+
+def starkv_dense_evict(plan: DensePlan, weights, ctx_len, keep: int, sink: int, recent: int,
+                       table_out=None, weights_out=None, ctx_out=None, stream=None) -> None:
+    _check(lib().starkv_dense_evict(plan.handle, _ptr(weights), _ptr(ctx_len), keep, sink, recent,
+                                    _ptr(table_out), _ptr(weights_out), _ptr(ctx_out),
+                                    _stream(stream)))
 
 
 def starkv_status_string(status: int) -> str:

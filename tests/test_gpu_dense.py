@@ -1,0 +1,820 @@
+"""Uncompressed layers on the GPU against float64: rotary positions, the 8-bit cache, attention
+over it and eviction.
+
+Tolerances.  A result in a type with step eps is off by at most eps/2 of itself from its rounding.
+Rotation: two products and a sum in fp32 with cos and sin off by 2^-23 (their argument's
+rounding, 2^-24 pi, and theirs): 2^-21 (|x_p| + |x_q|) gain.  Attention: with X = max sum |q k|
+scale over the tokens seen, a score is off by at most 2 X (d + 8) 2^-24; each probability is
+rounded to fp16 (2^-11), sums of N terms in fp32 (2^-24 (N/16 + 64): at least 16 partial sums);
+an output is off by the sum of these times sum p |v|, and what fp16 drops, 2^-29 of the largest."""
+import math
+
+import numpy as np
+import pytest
+
+from _helpers import say
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+import _dense_ref as R  # noqa: E402
+from paper_2606_08382_amd import starkv as S  # noqa: E402
+
+DT = {"f16": S.DT_F16, "bf16": S.DT_BF16, "f32": S.DT_F32}
+TT = {"f16": torch.float16, "bf16": torch.bfloat16, "f32": torch.float32}
+
+
+def rand(*shape, seed=0, dtype=torch.float64):
+    g = torch.Generator().manual_seed(seed)
+    return torch.randn(*shape, generator=g, dtype=torch.float64).to(dtype)
+
+
+def ints(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+# ------------------------------------------------------------------------ rotary positions
+
+def check_rope(got, x, want, gain, dtype):
+    eps = torch.finfo(TT[dtype]).eps
+    room = x.abs().amax(-1, keepdim=True) * 2 * gain * 2.0 ** -21
+    err = (got.double().cpu() - want).abs()
+    assert (err <= eps / 2 * want.abs() + room * (1 + eps) + 2.0 ** -25).all(), err.max()
+
+
+ROPES = [  # d, R, layout, scaling, factor, L0, dtype
+    (128, 128, "half", 0, 1, 0, "bf16"), (128, 128, "half", 3, 8, 8192, "bf16"),
+    (128, 96, "half", 4, 16, 4096, "f16"), (64, 64, "half", 1, 4, 0, "f32"),
+    (64, 64, "half", 2, 4, 0, "f32"), (128, 128, "interleaved", 4, 8, 8192, "bf16"),
+    (128, 96, "interleaved", 2, 8, 0, "f32"), (64, 32, "interleaved", 1, 3, 0, "f16"),
+    (128, 20, "half", 0, 1, 0, "bf16"), (128, 18, "interleaved", 3, 2, 500, "f16"),
+    (6, 2, "half", 0, 1, 0, "f32"), (512, 512, "half", 0, 1, 0, "bf16"),
+    (80, 80, "interleaved", 0, 1, 0, "bf16"), (36, 24, "half", 4, 2, 700, "f32"),
+]
+
+
+@pytest.mark.parametrize("n,heads", [(1, 1), (7, 5), (300, 9)])
+@pytest.mark.parametrize("case", ROPES)
+def test_rope(case, n, heads):
+    from paper_2606_08382_amd.device import Rope
+    d, rot, layout, scaling, factor, L0, dtype = case
+    say(f"rope {case} n={n} heads={heads}")
+    rope = Rope(d, 1e4, rot, S.ROPE_HALF if layout == "half" else S.ROPE_INTERLEAVED, scaling,
+                factor, L0, dtype=DT[dtype])
+    x = rand(2, n, heads, d, seed=n, dtype=TT[dtype])
+    pos = torch.randint(0, 1 << 20, (2, n), generator=torch.Generator().manual_seed(3),
+                        dtype=torch.int32)
+    pos[0, 0], pos[-1, -1] = 0, 2 ** 31 - 1
+    if n > 2:
+        pos[1, 0] = -77
+    f = R.rope_turns(rot, 1e4, scaling, factor, L0)
+    gain = 0.1 * math.log(factor) + 1 if scaling == 4 else 1.0
+    # fp64 angles of the largest position are off by 2^31 2^-53 of a turn; float64 cos by as much
+    y = rope(x.cuda(), pos.cuda())
+    check_rope(y, x.double(), R.rope(x.double(), pos, f, layout != "half", gain), gain, dtype)
+    z = rope(x.cuda(), pos.cuda(), inverse=True)
+    check_rope(z, x.double(), R.rope(x.double(), pos, f, layout != "half", gain, True), gain, dtype)
+
+
+@pytest.mark.parametrize("layout", [S.ROPE_HALF, S.ROPE_INTERLEAVED])
+def test_rope_strides_and_in_place(layout):
+    from paper_2606_08382_amd.device import Rope
+    rope = Rope(64, 1e4, layout=layout)
+    f = R.rope_turns(64, 1e4, 0)
+    pos = torch.arange(10, dtype=torch.int32).view(2, 5) * 1000
+    base = rand(2, 5, 8, 64, dtype=torch.bfloat16)
+    want = R.rope(base.double(), pos, f, layout == 1)
+
+    def check(y, sel=slice(None)):
+        check_rope(y, base[:, :, sel].double(), want[:, :, sel], 1.0, "bf16")
+    x = base.cuda()
+    # heads of a fused row, one of them in place; the others stay
+    y = x.clone()
+    rope(y[:, :, 2:5], pos.cuda(), out=y[:, :, 2:5])
+    check(y[:, :, 2:5], slice(2, 5))
+    assert torch.equal(y[:, :, :2], x[:, :, :2]) and torch.equal(y[:, :, 5:], x[:, :, 5:])
+    # head-major input, token-major output, and the other way round
+    hm = x.transpose(1, 2).contiguous().transpose(1, 2)
+    check(rope(hm, pos.cuda(), out=torch.empty_like(x)))
+    out = torch.empty(2, 8, 5, 64, dtype=torch.bfloat16, device="cuda").transpose(1, 2)
+    check(rope(x, pos.cuda(), out=out))
+    # rows that are not 16-byte aligned
+    odd = torch.empty(2, 5, 8, 67, dtype=torch.bfloat16, device="cuda")[..., 1:65]
+    odd.copy_(x)
+    check(rope(odd, pos.cuda()))
+    flat = torch.empty(x.numel() + 1, dtype=torch.bfloat16, device="cuda")[1:].view(x.shape)
+    check(rope(x, pos.cuda(), out=flat))
+    # a broadcast input; three dimensions; bit patterns
+    one = rope(x[:, :, :1].expand(2, 5, 8, 64), pos.cuda())
+    assert torch.equal(one, one[:, :, :1].expand_as(one))
+    check(rope(x.view(10, 8, 64), pos.view(-1).cuda()).view(2, 5, 8, 64))
+    check(rope(x.view(torch.int16), pos.cuda()).view(torch.bfloat16))
+    assert rope(x[:, :0], pos[:, :0].cuda()).shape == (2, 0, 8, 64)
+
+
+@pytest.mark.parametrize("layout", [S.ROPE_HALF, S.ROPE_INTERLEAVED])
+def test_rope_inverse_is_the_gradient(layout):
+    from paper_2606_08382_amd.device import Rope
+    rope = Rope(32, 1e4, 24, layout, S.ROPE_YARN, 4.0, 256, dtype=S.DT_F32)
+    f = R.rope_turns(24, 1e4, 4, 4.0, 256)
+    gain = 0.1 * math.log(4.0) + 1
+    pos = torch.arange(6, dtype=torch.int32).view(1, 6) * 37
+    x = rand(1, 6, 3, 32, seed=1).requires_grad_()
+    up = rand(1, 6, 3, 32, seed=2, dtype=torch.float32)
+    (R.rope(x, pos, f, layout == 1, gain) * up.double()).sum().backward()
+    got = rope(up.cuda(), pos.cuda(), inverse=True)
+    check_rope(got, up.double(), x.grad, gain, "f32")
+    # and against differences: the map is linear, so a difference of any step is its derivative
+    e = torch.zeros(1, 6, 3, 32)
+    e[0, 4, 1, 3] = 1.0
+    diff = (rope(e.cuda(), pos.cuda()).double().cpu() * up.double()).sum()
+    assert abs(diff - x.grad[0, 4, 1, 3]) <= 32 * 2.0 ** -21 * gain * up.abs().max()
+
+
+# --------------------------------------------------------------------------------- cache
+
+def layer_of(batch, n_q, n_kv, d, cap, code=0, T=64, dtype="bf16", **kw):
+    from paper_2606_08382_amd.device import DenseLayer
+    layer = DenseLayer(batch, n_q, n_kv, d, cap, code=code, block_tokens=T, dtype=DT[dtype], **kw)
+    layer.cache.fill_(0xff)                  # NaN codes, scales and rows wherever nothing is written
+    return layer
+
+
+def shuffled_table(batch, n_kv, cap, T, extra=3, seed=0):
+    J = -(-cap // T)
+    n = batch * n_kv * J
+    g = torch.Generator().manual_seed(seed)
+    t = torch.randperm(n + extra, generator=g)[:n].to(torch.int32).view(batch, n_kv, J).cuda()
+    return dict(block_table=t, n_blocks=n + extra)
+
+
+def block_of(layer, b, g, j):
+    """Key and value codes [T][d] (as numbers) and scales of a block, from the documented layout."""
+    L = S.starkv_dense_cache_layout(layer.plan)
+    T, d = layer.block_tokens, layer.head_dim
+    raw = layer.cache.cpu()
+    e = int(layer.table[b, g, j])
+    c = raw[e * L.block_bytes:(e + 1) * L.block_bytes].view(2, T // 16, d // 64, 4, 16, 16)
+    k = c[0].permute(0, 3, 1, 2, 4).reshape(T, d)              # [sub][grp][a][tau][c]
+    v = c[1].view(T // 16, d // 64, 4, 16, 4, 4)               # [sub][grp][a][c][j][r]
+    v = v.permute(0, 2, 5, 1, 4, 3).reshape(T, d)
+    s = raw[L.scale_offset + 8 * e:L.scale_offset + 8 * e + 8].view(torch.float32)
+    if layer.cfg.code == 0:
+        return k.double() - 128, v.double() - 128, s
+    f = torch.float8_e4m3fn
+    return (k.contiguous().view(f).double(), v.contiguous().view(f).double(), s)
+
+
+def read_all(layer, ctx, start=None, n=None, dtype=torch.float32):
+    n = layer.capacity if n is None else n
+    shape = (layer.batch, n, layer.n_kv, layer.head_dim)
+    k = torch.full(shape, 7.0, dtype=dtype, device="cuda")
+    v = torch.full(shape, 7.0, dtype=dtype, device="cuda")
+    layer.read(ctx, ints([0] * layer.batch) if start is None else start, k, v)
+    return k, v
+
+
+def kv(batch, n, n_kv, d, dtype="bf16", seed=0):
+    k, v = rand(2, batch, n, n_kv, d, seed=seed, dtype=TT[dtype])
+    k[..., 3] *= 8
+    return k, v
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("code", [0, 1])
+@pytest.mark.parametrize("d,T", [(128, 64), (64, 16), (128, 16), (64, 128), (128, 32), (128, 128)])
+def test_append_codes_and_read(d, T, code, dtype):
+    say(f"append d={d} T={T} code={code} {dtype}")
+    lens, cap = [3 * T + 5, 0, T - 1, 2 * T], 4 * T
+    layer = layer_of(4, 4, 2, d, cap, code, T, dtype, **shuffled_table(4, 2, cap, T))
+    k, v = kv(4, max(lens), 2, d, dtype)
+    k[0, :T, 1] = 0                                            # a block of zeros
+    layer.append(k.cuda(), v.cuda(), ints([0] * 4), n_new=ints(lens))
+    for b, n in enumerate(lens):
+        for g in range(2):
+            for j in range(n // T):
+                rows = slice(j * T, (j + 1) * T)
+                ck, cv, s = block_of(layer, b, g, j)
+                for got, x, sc in ((ck, k, s[0]), (cv, v, s[1])):
+                    want, ws = R.quantize(x[b, rows, g], code)
+                    assert torch.equal(sc, ws) and torch.equal(got, want), (b, g, j)
+    ks, vs = read_all(layer, ints(lens))
+    for b, n in enumerate(lens):
+        for g in range(2):
+            for got, x in ((ks, k), (vs, v)):
+                want = torch.zeros(cap, d, dtype=torch.float64)
+                want[:n] = R.cached(x[b, :n, g], code, T)
+                assert torch.equal(got[b, :, g].cpu(), want.float()), (b, g)
+
+
+@pytest.mark.parametrize("code", [0, 1])
+def test_append_borders(code):
+    """Quotients on and next to the borders of codes, over many scales: every code exact."""
+    T, d = 16, 64
+    g = R.grid(code)
+    mid = (g[1:] + g[:-1]) / 2
+    vals = torch.cat([mid, g[1:], -mid])
+    blocks = []
+    for i, top in enumerate([1.0, 127.0, 448.0, 1.9921875, 3.140625, 2.0 ** -9, 2.0 ** -120, 1e-38,
+                             2.0 ** -132, 1e38, 3.3e38, 1.0078125 * 2.0 ** -70]):
+        s = float(torch.tensor(top / R.TOP[code]).float())
+        for off in range(0, len(vals), T * d - 1):
+            x = torch.zeros(T * d, dtype=torch.float64)
+            part = (vals[off:off + T * d - 1] * s)
+            x[:len(part)] = part.clamp(-top, top)
+            x[-1] = top
+            blocks.append(x.view(T, d))
+    x = torch.cat(blocks).to(torch.bfloat16)[None, :, None]
+    n = x.shape[1]
+    layer = layer_of(1, 1, 1, d, n, code, T)
+    layer.append(x.cuda(), x.cuda(), ints([0]))
+    for j in range(n // T):
+        ck, cv, s = block_of(layer, 0, 0, j)
+        want, ws = R.quantize(x[0, j * T:(j + 1) * T, 0], code)
+        assert torch.equal(s, ws.expand(2)), (j, s, ws)
+        assert torch.equal(ck, want) and torch.equal(cv, want), j
+
+
+def test_append_all_16bit_patterns():
+    """Every finite fp16 and bf16 value against scales of its own size and larger."""
+    T, d = 16, 64
+    for dtype, top in (("f16", 0x7c00), ("bf16", 0x7f80)):
+        x = torch.arange(0, top // 1024 * 1024, dtype=torch.int32).to(torch.int16)
+        x = x.view(TT[dtype]).view(1, -1, 1, d)
+        n = x.shape[1]
+        for code in (0, 1):
+            layer = layer_of(1, 1, 1, d, n, code, T, dtype)
+            y = x.flip(3)
+            y[:, ::2] *= -1
+            layer.append(x.cuda(), y.contiguous().cuda(), ints([0]))
+            ks, vs = read_all(layer, ints([n]))
+            assert torch.equal(ks[0, :, 0].cpu(), R.cached(x[0, :, 0], code, T).float())
+            assert torch.equal(vs[0, :, 0].cpu(), R.cached(y[0, :, 0], code, T).float())
+
+
+@pytest.mark.parametrize("code", [0, 1])
+def test_append_nonfinite(code):
+    T, d = 32, 128
+    k, v = kv(1, 4 * T + 3, 2, d)
+    k[0, 5, 0, 7], k[0, T + 1, 1, 0], v[0, 2 * T, 0, 1] = math.nan, math.inf, -math.inf
+    layer = layer_of(1, 2, 2, d, 5 * T, code, T)
+    layer.append(k.cuda(), v.cuda(), ints([0]))
+    ks, vs = read_all(layer, ints([4 * T + 3]), n=4 * T + 3)
+    for got, x in ((ks, k), (vs, v)):
+        for g in range(2):
+            want = R.cached(x[0, :, g], code, T).float()
+            assert torch.equal(torch.isnan(got[0, :, g].cpu()), torch.isnan(want))
+            assert torch.equal(torch.nan_to_num(got[0, :, g].cpu()), torch.nan_to_num(want))
+
+
+@pytest.mark.parametrize("T", [16, 64])
+def test_append_does_not_depend_on_chunks(T):
+    n, d = 5 * T + 7, 128
+    k, v = kv(2, n, 2, d)
+    whole = layer_of(2, 2, 2, d, n, 0, T)
+    whole.append(k.cuda(), v.cuda(), ints([0, 0]))
+    want = read_all(whole, ints([n, n]))
+    for sizes in ([1], [3], [T - 1], [T + 1, 1, 2], [2 * T + 5, 7]):
+        layer = layer_of(2, 2, 2, d, n, 0, T)
+        t = i = 0
+        while t < n:
+            m = min(sizes[i % len(sizes)], n - t)
+            layer.append(k[:, t:t + m].cuda(), v[:, t:t + m].cuda(), ints([t, t]))
+            t, i = t + m, i + 1
+        got = read_all(layer, ints([n, n]))
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]), sizes
+
+
+def test_append_takes_tokens_back():
+    T, d = 16, 64
+    g = torch.Generator().manual_seed(5)
+    layer = layer_of(1, 1, 1, d, 20 * T, 1, T)
+    rows_k, rows_v = torch.zeros(0, 1, d), torch.zeros(0, 1, d)
+    n = lowest = 0
+    for step in range(60):
+        m = int(torch.randint(1, T + 4, (1,), generator=g))
+        m = min(m, 20 * T - n)
+        if m == 0:
+            break
+        k, v = kv(1, m, 1, d, seed=step)
+        layer.append(k.cuda(), v.cuda(), ints([n]))
+        rows_k, rows_v = torch.cat([rows_k[:n], k[0]]), torch.cat([rows_v[:n], v[0]])
+        n += m
+        ks, vs = read_all(layer, ints([n]), n=n)
+        assert torch.equal(ks[0, :, 0].cpu(), R.cached(rows_k[:, 0], 1, T).float()), step
+        assert torch.equal(vs[0, :, 0].cpu(), R.cached(rows_v[:, 0], 1, T).float()), step
+        # back as far as the 16-bit rows reach: the furthest token's block and the one before
+        lowest = max(lowest, ((n - 1) // T - 1) * T)
+        n = int(torch.randint(max(lowest, n - T), n + 1, (1,), generator=g))
+    # and to any multiple of T
+    k, v = kv(1, 2 * T + 3, 1, d, seed=99)
+    layer.append(k.cuda(), v.cuda(), ints([2 * T]))
+    ks, vs = read_all(layer, ints([4 * T + 3]), n=4 * T + 3)
+    want = torch.cat([rows_k[:2 * T, 0], k[0, :, 0]])
+    assert torch.equal(ks[0, :, 0].cpu(), R.cached(want, 1, T).float())
+
+
+def test_append_strides_capacity_and_table():
+    """Strided and unaligned rows; tokens outside the capacity and blocks outside the pool are
+    dropped, everything else of the cache stays as it was."""
+    T, d, cap = 16, 64, 3 * 16 + 5
+    table = shuffled_table(2, 2, cap, T, extra=2)
+    layer = layer_of(2, 2, 2, d, cap, 0, T, **table)
+    k, v = kv(2, cap, 2, d)
+    fused = torch.empty(2, cap, 7, d, dtype=torch.bfloat16, device="cuda")
+    fused[:, :, 1:3], fused[:, :, 4:6] = k.cuda(), v.cuda()
+    layer.append(fused[:, :, 1:3], fused[:, :, 4:6], ints([0, 0]))
+    want = read_all(layer, ints([cap, cap]))
+    for b in range(2):
+        assert torch.equal(want[0][b, :, 1].cpu(), R.cached(k[b, :, 1], 0, T).float())
+    odd = torch.empty(2, 2, cap, d + 1, dtype=torch.bfloat16, device="cuda")[..., 1:]
+    odd.copy_(k.transpose(1, 2))
+    other = layer_of(2, 2, 2, d, cap, 0, T, **table)
+    other.append(odd.transpose(1, 2), v.cuda(), ints([0, 0]))
+    got = read_all(other, ints([cap, cap]))
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    # tokens before 0 and from the capacity on
+    big_k, big_v = kv(2, cap + 20, 2, d, seed=4)
+    big_k[:, 9:9 + cap], big_v[:, 9:9 + cap] = k, v
+    other = layer_of(2, 2, 2, d, cap, 0, T, **table)
+    other.append(big_k.cuda(), big_v.cuda(), ints([-9, -9]))
+    got = read_all(other, ints([cap, cap]))
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    before = other.cache.clone()
+    for pos in ([cap, 2 ** 31 - 1], [-2 ** 31, -cap - 20]):
+        other.append(big_k.cuda(), big_v.cuda(), ints(pos))
+    other.append(big_k.cuda(), big_v.cuda(), ints([0, 0]), n_new=ints([0, -5]))
+    assert torch.equal(other.cache, before)
+    # entries outside the pool
+    layer.table[0, 0, 1], layer.table[1, 1, 0] = -1, layer.cfg.n_blocks
+    before = layer.cache.clone()
+    L = S.starkv_dense_cache_layout(layer.plan)
+    layer.append(big_k[:, :cap].cuda(), big_v[:, :cap].cuda(), ints([0, 0]))
+    used = set(layer.table.flatten().tolist())
+    for e in range(layer.cfg.n_blocks):
+        same = torch.equal(layer.cache[e * L.block_bytes:(e + 1) * L.block_bytes],
+                           before[e * L.block_bytes:(e + 1) * L.block_bytes])
+        entry = (layer.table == e).nonzero()
+        whole = len(entry) and int(entry[0, 2]) < cap // T
+        assert same == (e not in used or not whole), e
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16, torch.float32])
+def test_read_ranges_and_types(dtype):
+    T, d, n = 32, 128, 3 * 32 + 9
+    k, v = kv(2, n, 3, d)
+    layer = layer_of(2, 3, 3, d, 5 * 32, 1, T)
+    layer.append(k.cuda(), v.cuda(), ints([0, 0]))
+    full = torch.stack([torch.stack([R.cached(k[b, :, g], 1, T) for g in range(3)], 1)
+                        for b in range(2)]).float()
+    for start, m in (([5, 90], 70), ([-20, 100], 64), ([n - 1, n], 1), ([2 ** 31 - 4, -2 ** 31], 3)):
+        shape = (2, 3, m, d)                           # head-major outputs
+        ko = torch.full(shape, 7.0, dtype=dtype, device="cuda").transpose(1, 2)
+        vo = torch.full(shape, 7.0, dtype=dtype, device="cuda").transpose(1, 2)
+        layer.read(ints([n, n - 3]), ints(start), ko, vo)
+        want = torch.zeros(2, m, 3, d)
+        for b, ctx in enumerate((n, n - 3)):
+            for i in range(m):
+                if 0 <= start[b] + i < ctx:
+                    want[b, i] = full[b, start[b] + i]
+        if ctx < n:                                     # (tokens of the unfinished block)
+            assert torch.equal(ko[0].cpu(), want[0].to(dtype))
+        assert torch.equal(ko[1].cpu(), want[1].to(dtype))
+
+
+# ------------------------------------------------------------------------------ attention
+
+def reference(k, v, q, ctx, q_len, code, T, scale=None):
+    """Per sequence and query head in float64: out, tolerance, block weights."""
+    B, n, H_q, d = q.shape
+    H = k.shape[2]
+    G, J = H_q // H, -(-max(max(ctx), 1) // T)
+    out = torch.zeros(B, n, H_q, d, dtype=torch.float64)
+    tol = torch.zeros_like(out)
+    w = torch.zeros(B, H, J, dtype=torch.float64)
+    eps = torch.finfo(q.dtype).eps
+    c = 1 / math.sqrt(d) if scale is None else scale
+    for b in range(B):
+        L, m = ctx[b], q_len[b]
+        if m == 0:
+            continue
+        for g in range(H):
+            K, V = R.cached(k[b, :L, g], code, T), R.cached(v[b, :L, g], code, T)
+            for i in range(g * G, (g + 1) * G):
+                o, a, big, p = R.attend(q[b, :m, i], K, V, c, L - m)
+                out[b, :m, i] = o
+                rel = 2.0 ** -11 + 4 * big * (d + 8) * 2.0 ** -24 + 2.0 ** -24 * (L / 16 + 64)
+                # (a block that is not finite has no part in the rows that are compared)
+                top = torch.nan_to_num(V.abs(), nan=0.0).amax() * L * 2.0 ** -29 if L else 0.0
+                tol[b, :m, i] = eps / 2 * o.abs() + (1 + eps) * (rel[:, None] * a + top) + 2.0 ** -25
+                per = torch.zeros(J * T, dtype=torch.float64)
+                per[:L] = p.sum(0)
+                w[b, g] += per.view(J, T).sum(-1)
+    return out, tol, w
+
+
+def run_attend(ctx, n=1, n_q=8, n_kv=2, d=128, code=0, T=64, dtype="bf16", q_len=None, cap=None,
+               k_scale=1.0, weights=None, seed=0, scale=0.0, edit=None):
+    B = len(ctx)
+    say(f"attend ctx={ctx} n={n} heads={n_q}/{n_kv} d={d} code={code} T={T} {dtype} q_len={q_len}")
+    cap = max(max(ctx), 1) if cap is None else cap
+    layer = layer_of(B, n_q, n_kv, d, cap, code, T, dtype, softmax_scale=scale,
+                     **shuffled_table(B, n_kv, cap, T, seed=seed))
+    k, v = kv(B, max(max(ctx), 1), n_kv, d, dtype, seed=seed)
+    k = (k.double() * k_scale).to(TT[dtype])
+    if edit:
+        edit(k, v)
+    q = rand(B, n, n_q, d, seed=seed + 1, dtype=TT[dtype])
+    layer.append(k.cuda(), v.cuda(), ints([0] * B), n_new=ints(ctx))
+    out = torch.full(q.shape, 5.0, dtype=TT[dtype], device="cuda")
+    w0 = None
+    if weights is None:
+        weights = n * (n_q // n_kv) <= 64
+    if weights:
+        w0 = layer.new_weights()
+        w0 += 0.5
+    layer.attend(q.cuda(), ints(ctx), q_len=None if q_len is None else ints(q_len), weights=w0,
+                 out=out)
+    torch.cuda.synchronize()
+    m = [n] * B if q_len is None else q_len
+    ref, tol, w = reference(k, v, q, ctx, m, code, T, scale or None)
+    got = out.double().cpu()
+    for b in range(B):
+        err = (got[b, :m[b]] - ref[b, :m[b]]).abs()
+        assert torch.isfinite(got[b]).all(), b
+        assert (err <= tol[b, :m[b]]).all(), (b, (err / tol[b, :m[b]]).max())
+        assert (got[b, m[b]:] == 5.0).all()                  # rows of no query token
+    if weights:
+        J = w.shape[2]
+        # relative to the rows' whole weight: scores' errors as above, sums in fp32
+        rows = n * (n_q // n_kv)
+        err = (w0.double().cpu()[:, :, :J] - 0.5 - w).abs()
+        assert (err <= 1e-5 * w + rows * 2.0 ** -23).all(), err.max()
+        assert (w0[:, :, J:] == 0.5).all()
+    return layer, k, v, q, out
+
+
+LENGTHS = [[1], [15, 16, 17], [63, 64, 65, 0], [127, 128, 129], [200, 1000, 31, 2500]]
+
+
+@pytest.mark.parametrize("d,code,dtype,T", [(128, 0, "bf16", 64), (128, 1, "bf16", 32),
+                                            (64, 0, "f16", 16), (64, 1, "f16", 128),
+                                            (128, 0, "f16", 16), (128, 1, "bf16", 128)])
+@pytest.mark.parametrize("ctx", LENGTHS)
+def test_decode(ctx, d, code, dtype, T):
+    run_attend(ctx, d=d, code=code, dtype=dtype, T=T)
+
+
+@pytest.mark.parametrize("n_q,n_kv", [(1, 1), (6, 2), (5, 1), (16, 1), (32, 2), (17, 1), (64, 1),
+                                      (33, 1), (7, 7), (48, 16)])
+def test_decode_head_groups(n_q, n_kv):
+    run_attend([77, 300], n_q=n_q, n_kv=n_kv, d=64, T=16)
+    run_attend([77, 300], n_q=n_q, n_kv=n_kv, code=1, T=32, dtype="f16")
+
+
+@pytest.mark.parametrize("n,n_q,n_kv", [(2, 8, 2), (5, 8, 1), (7, 3, 1), (16, 4, 2), (40, 2, 2),
+                                        (65, 1, 1), (130, 4, 2), (33, 64, 16)])
+@pytest.mark.parametrize("T,code,dtype,d", [(16, 0, "bf16", 128), (64, 1, "f16", 64),
+                                            (128, 0, "f16", 128)])
+def test_several_query_tokens(n, n_q, n_kv, T, code, dtype, d):
+    """Causal among the last tokens; contexts shorter than the query tokens leave rows empty;
+    padded batches."""
+    ctx = [n + 200, n, max(n - 3, 1), n + 17]
+    run_attend(ctx, n=n, n_q=n_q, n_kv=n_kv, T=T, code=code, dtype=dtype, d=d)
+    run_attend(ctx, n=n, n_q=n_q, n_kv=n_kv, T=T, code=code, dtype=dtype, d=d,
+               q_len=[n, 0, n - 1, 1])
+
+
+def test_large_scores_and_scales():
+    run_attend([700, 130], k_scale=40.0)                     # one token takes nearly all
+    run_attend([700, 130], k_scale=3000.0, dtype="bf16", code=1)
+    run_attend([700, 130], k_scale=1e-30)
+    run_attend([300, 64], scale=2.5, dtype="f16")
+
+    def uneven(k, v):                                        # value scales 2^-60 .. 2^60
+        for j in range(0, v.shape[1], 64):
+            v[:, j:j + 64] = (v[:, j:j + 64].double() * 2.0 ** ((j // 64 * 37) % 121 - 60)).bfloat16()
+    run_attend([900, 450], edit=uneven)
+
+    def zeros(k, v):
+        v[:, :128] = 0
+        k[:, 64:192] = 0
+    run_attend([300, 200], edit=zeros)
+    run_attend([300, 200], edit=lambda k, v: v.zero_(), code=1)
+
+
+def test_query_extremes():
+    """Queries near the ends of their types; a row with an infinity or NaN stays alone."""
+    for dtype, top, low in (("bf16", 2.0 ** 120, 2.0 ** -120), ("f16", 60000.0, 2.0 ** -20)):
+        layer, k, v, q, _ = run_attend([333], dtype=dtype, n_q=4, n_kv=2)
+        want, tol, _ = reference(k, v, q, [333], [1], 0, 64)
+        for mul in (top, low):
+            # keys cannot follow, so compare with a scale that undoes the factor
+            s = mul / float(q.abs().max()) * 0.5
+            s = 2.0 ** math.floor(math.log2(s))
+            from paper_2606_08382_amd.device import DenseLayer
+            other = DenseLayer(1, 4, 2, 128, 333, dtype=DT[dtype],
+                               softmax_scale=1 / math.sqrt(128) / s)
+            other.append(k.cuda(), v.cuda(), ints([0]))
+            got = other.attend((q.double() * s).to(TT[dtype]).cuda(), ints([333])).double().cpu()
+            if dtype == "bf16" or mul == top:
+                assert ((got - want).abs() <= tol).all(), (dtype, mul)
+        bad = q.clone()
+        bad[0, 0, 1, 5], bad[0, 0, 3, 0] = math.inf, math.nan
+        got = layer.attend(bad.cuda(), ints([333])).double().cpu()
+        assert torch.isnan(got[0, 0, 1]).all() and torch.isnan(got[0, 0, 3]).all()
+        for i in (0, 2):
+            assert ((got - want).abs()[0, 0, i] <= tol[0, 0, i]).all()
+
+
+def test_nonfinite_blocks_reach_only_what_attends_to_them():
+    T = 32
+
+    def edit(k, v):
+        v[0, 4 * T + 3, 0, 9] = math.nan                     # finished block 4 of KV head 0
+        k[0, 6 * T, 1, 0] = math.inf                         # block 6 of KV head 1
+    ctx, n = 8 * T + 5, 5 * T
+    layer = layer_of(1, 2, 2, 64, ctx, 0, T)
+    k, v = kv(1, ctx, 2, 64)
+    edit(k, v)
+    layer.append(k.cuda(), v.cuda(), ints([0]))
+    q = rand(1, n, 2, 64, seed=3, dtype=torch.bfloat16)
+    got = layer.attend(q.cuda(), ints([ctx])).double().cpu()[0]
+    first = ctx - n
+    ref, tol, _ = reference(k, v, q, [ctx], [n], 0, T)
+    for j in range(n):
+        pos = first + j
+        # the block's scale is NaN, so is what sees any of its tokens
+        assert torch.isnan(got[j, 0]).all() == (pos >= 4 * T), j
+        assert torch.isnan(got[j, 1]).all() == (pos >= 6 * T), j
+        for h, lim in ((0, 4 * T), (1, 6 * T)):
+            if pos < lim:
+                assert ((got[j, h] - ref[0, j, h]).abs() <= tol[0, j, h]).all()
+
+
+def test_attend_strides():
+    layer, k, v, q, out = run_attend([200, 90], n=3, n_q=4, n_kv=2)
+    ctx = ints([200, 90])
+    want = out.clone()
+    fused = torch.full((2, 3, 9, 128), 3.0, dtype=torch.bfloat16, device="cuda")
+    fused[:, :, 2:6] = q.cuda()
+    o = torch.full((2, 3, 9, 128), 3.0, dtype=torch.bfloat16, device="cuda")
+    layer.attend(fused[:, :, 2:6], ctx, out=o[:, :, 1:5])
+    assert torch.equal(o[:, :, 1:5], want)
+    assert (o[:, :, 0] == 3).all() and (o[:, :, 5:] == 3).all()
+    hm = q.cuda().transpose(1, 2).contiguous().transpose(1, 2)
+    oh = torch.empty(2, 4, 3, 128, dtype=torch.bfloat16, device="cuda").transpose(1, 2)
+    assert torch.equal(layer.attend(hm, ctx, out=oh), want)
+    odd = torch.empty(2, 3, 4, 129, dtype=torch.bfloat16, device="cuda")[..., 1:]
+    odd.copy_(q)
+    oo = torch.empty(2, 3, 4, 131, dtype=torch.bfloat16, device="cuda")[..., 3:]
+    assert torch.equal(layer.attend(odd, ctx, out=oo), want)
+    # one token without its dimension; a smaller max_ctx that still covers the lengths
+    one = layer.attend(q[:, 2].cuda(), ctx)
+    assert one.shape == (2, 4, 128)
+    err = (one.double() - want[:, 2].double()).abs()
+    assert (err <= 2.0 ** -7 * want[:, 2].double().abs() + 2.0 ** -9).all()
+    assert (layer.attend(q.cuda(), ctx, max_ctx=90)[1] == want[1]).all()
+    # shared blocks: sequence 1 reads sequence 0's
+    layer.table[1, :, :1] = layer.table[0, :, :1]
+    got = layer.attend(q.cuda(), ctx)
+    k[1, :64], v[1, :64] = k[0, :64], v[0, :64]
+    ref, tol, _ = reference(k, v, q, [200, 90], [3, 3], 0, 64)
+    assert ((got.double().cpu() - ref).abs() <= tol).all()
+
+
+def test_lengths_are_clamped():
+    layer, k, v, q, out = run_attend([100, 60])
+    got = layer.attend(q.cuda(), ints([2 ** 31 - 1, -5]), max_ctx=100)
+    assert torch.equal(got[0], out[0]) and (got[1] == 0).all()
+
+
+def test_offsets_beyond_32_bits():
+    """Blocks at the end of a pool of more than 4 GiB."""
+    from paper_2606_08382_amd.device import DenseLayer
+    T, d, n_blocks = 128, 128, 180000                        # 32 KiB each
+    table = (n_blocks - 1 - torch.arange(2 * 3, dtype=torch.int32)).view(1, 2, 3).cuda()
+    layer = DenseLayer(1, 4, 2, d, 3 * T, block_tokens=T, n_blocks=n_blocks, block_table=table)
+    assert layer.cache.numel() > 1 << 32
+    k, v = kv(1, 3 * T - 2, 2, d)
+    q = rand(1, 1, 4, d, seed=2, dtype=torch.bfloat16)
+    layer.append(k.cuda(), v.cuda(), ints([0]))
+    got = layer.attend(q.cuda(), ints([3 * T - 2]))
+    ref, tol, _ = reference(k, v, q, [3 * T - 2], [1], 0, T)
+    assert ((got.double().cpu() - ref).abs() <= tol).all()
+    ks, _ = read_all(layer, ints([3 * T - 2]), n=3 * T - 2)
+    assert torch.equal(ks[0, :, 1].cpu(), R.cached(k[0, :, 1], 0, T).float())
+
+
+@pytest.mark.parametrize("B", [3, 70])
+def test_many_ragged_sequences_and_long_contexts(B):
+    """Work items over ragged lengths: more than one wave's worth of sequences, long ones."""
+    g = torch.Generator().manual_seed(B)
+    ctx = torch.randint(0, 400, (B,), generator=g).tolist()
+    ctx[1], ctx[-1] = 20000 if B == 3 else 3000, 0
+    run_attend(ctx, n_q=4, n_kv=1, d=64, T=32, code=1)
+
+
+def test_same_bytes_again_and_from_other_streams():
+    layer, k, v, q, out = run_attend([900, 333], n_q=16, n_kv=2)
+    qg, ctx = q.cuda(), ints([900, 333])
+    w = layer.new_weights()
+    a = layer.attend(qg, ctx, weights=w)
+    w2 = layer.new_weights()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        b = layer.attend(qg, ctx, weights=w2)
+    side.synchronize()
+    assert torch.equal(a, b) and torch.equal(w, w2)
+    # two calls at once, each with a workspace of its own
+    other = torch.empty_like(layer.workspace(1))
+    torch.cuda.synchronize()
+    for _ in range(5):
+        with torch.cuda.stream(side):
+            c = layer.attend(qg, ctx, ws=other)
+        e = layer.attend(qg, ctx)
+        torch.cuda.synchronize()
+        assert torch.equal(c, a) and torch.equal(e, a)
+
+
+# --------------------------------------------------------------------------------- evict
+
+def check_evict(w, table, ctx, T, keep, sink, recent, got):
+    t, wo, co = (x.cpu() for x in got)
+    for b, L in enumerate(ctx):
+        for h in range(w.shape[1]):
+            rt, rw, rc = R.evict(w[b, h].tolist(), table[b, h].tolist(), L, T, keep, sink, recent)
+            assert t[b, h].tolist() == rt, (b, h)
+            assert torch.equal(torch.nan_to_num(wo[b, h], nan=-1.0),
+                               torch.nan_to_num(torch.tensor(rw), nan=-1.0)), (b, h)
+            assert int(co[b]) == rc
+
+
+@pytest.mark.parametrize("cap,T,ctx,keep,sink,recent", [
+    (64, 16, [64, 63, 0, 16], 1, 0, 0), (64, 16, [64, 50, 17, 33], 2, 1, 1),
+    (1000, 16, [1000, 999, 500, 3], 10, 2, 5), (1000, 16, [1000, 640, 161, 176], 10, 0, 10),
+    (1000, 16, [1000, 640, 161, 176], 10, 10, 0), (1000, 32, [1000, 1000, 800, 30], 100, 1, 1),
+    (40000, 16, [40000, 39999, 20011, 16384], 700, 4, 30), (40000, 16, [40000] * 4, 2499, 0, 0),
+    (100000, 16, [100000, 65536, 65535, 9], 4096, 1, 1000),
+    (524288, 16, [524288, 300001, 524287, 20], 1000, 3, 3),
+])
+def test_evict(cap, T, ctx, keep, sink, recent):
+    say(f"evict cap={cap} T={T} ctx={ctx} keep={keep} sink={sink} recent={recent}")
+    from paper_2606_08382_amd.device import DenseLayer
+    J = -(-cap // T)
+    g = torch.Generator().manual_seed(cap + keep)
+    table = torch.randperm(4 * 2 * J, generator=g).to(torch.int32).view(4, 2, J)
+    # (the pool itself is not touched: one block serves)
+    w = torch.exp(2 * torch.randn(4, 2, J, generator=g))
+    w[1] = torch.round(w[1])                                 # ties
+    w[2, 0] = 0.0
+    w[2, 1, ::3] = math.nan
+    w[3, 0, ::2] = -0.0
+    w[3, 1, ::5], w[3, 1, 1::5] = math.inf, -1.5
+    layer = DenseLayer(4, 2, 2, 64, cap, block_tokens=T, n_blocks=1, block_table=table.cuda())
+    out = (torch.empty_like(layer.table), torch.full((4, 2, J), 9.0, device="cuda"), ints([7] * 4))
+    layer.evict(w.cuda(), ints(ctx), keep, sink, recent, *out)
+    check_evict(w, table, ctx, T, keep, sink, recent, out)
+    assert torch.equal(layer.table.cpu(), table)
+    # in place: the same
+    wg, cg = w.cuda(), ints(ctx)
+    got = layer.evict(wg, cg, keep, sink, recent)
+    assert got[0] is layer.table and got[1] is wg and got[2] is cg
+    assert torch.equal(got[0], out[0]) and torch.equal(got[2], out[2])
+    assert torch.equal(torch.nan_to_num(got[1], nan=-1.0), torch.nan_to_num(out[1], nan=-1.0))
+
+
+@pytest.mark.parametrize("T,code", [(16, 1), (64, 0)])
+def test_layer_over_many_steps(T, code):
+    """A layer as a model runs it: a prompt in chunks, then decode steps, with rotated queries and
+    keys, gathered weights and evictions; every step against float64."""
+    from paper_2606_08382_amd.device import Rope
+    B, n_q, n_kv, d, cap = 2, 6, 2, 64, 12 * T
+    rope = Rope(d, 1e4, scaling=S.ROPE_BANDS, factor=4.0, original_ctx=64)
+    f = R.rope_turns(d, 1e4, 3, 4.0, 64)
+    layer = layer_of(B, n_q, n_kv, d, cap, code, T, **shuffled_table(B, n_kv, cap, T))
+    w = layer.new_weights()
+    ctx = ints([0] * B)
+    seen = 0
+    rows = [[[] for _ in range(n_kv)] for _ in range(B)]      # what each head keeps: (k, v) tokens
+    g = np.random.default_rng(T)
+    for step in range(26):
+        n = int(g.integers(1, 2 * T)) if step < 4 else 1 + (step % 3)
+        if int(ctx.max()) + n > cap:
+            n = 1
+        x = rand(B, n, n_q + 2 * n_kv, d, seed=1000 + step, dtype=torch.bfloat16)
+        pos = (seen + torch.arange(n, dtype=torch.int32)).expand(B, n).contiguous()
+        xg = x.cuda()
+        rope(xg[:, :, :n_q + n_kv], pos.cuda(), out=xg[:, :, :n_q + n_kv])
+        want = R.rope(x[:, :, :n_q + n_kv].double(), pos, f, False)
+        check_rope(xg[:, :, :n_q + n_kv], x[:, :, :n_q + n_kv].double(), want, 1.0, "bf16")
+        layer.append(xg[:, :, n_q:n_q + n_kv], xg[:, :, n_q + n_kv:], ctx)
+        ctx = ctx + n
+        seen += n
+        gather = n * (n_q // n_kv) <= 64
+        w0 = w.clone()
+        out = layer.attend(xg[:, :, :n_q], ctx, weights=w if gather else None)
+        y, got = xg.cpu(), out.double().cpu()
+        for b in range(B):
+            for h in range(n_kv):
+                rows[b][h] += [(y[b, i, n_q + h], y[b, i, n_q + n_kv + h]) for i in range(n)]
+                k = torch.stack([r[0] for r in rows[b][h]])[None, :, None]
+                v = torch.stack([r[1] for r in rows[b][h]])[None, :, None]
+                q = y[b:b + 1, :, 3 * h:3 * h + 3]
+                L = int(ctx[b])
+                assert k.shape[1] == L
+                ref, tol, dw = reference(k, v, q, [L], [n], code, T)
+                assert ((got[b, :, 3 * h:3 * h + 3] - ref[0]).abs() <= tol[0]).all(), step
+                if gather:
+                    err = (w[b, h].cpu() - w0[b, h].cpu()).double()[:dw.shape[2]] - dw[0, 0]
+                    assert (err.abs() <= 1e-5 * (1 + w0[b, h].cpu()[:dw.shape[2]])).all(), step
+        if int(ctx.max()) > 9 * T:
+            before, wb = layer.table.cpu().clone(), w.cpu().clone()
+            n_old = int(ctx[0]) // T
+            layer.evict(w, ctx, 5, sink=1, recent=2)
+            for b in range(B):
+                for h in range(n_kv):
+                    order, _, left = R.evict(wb[b, h].tolist(), list(range(layer.blocks)),
+                                             int(n_old * T + len(rows[b][h]) % T), T, 5, 1, 2)
+                    keep = order[:left // T]
+                    tail = rows[b][h][n_old * T:]
+                    rows[b][h] = [r for j in keep for r in rows[b][h][j * T:(j + 1) * T]] + tail
+                    assert layer.table[b, h].tolist() == before[b, h][order].tolist()
+            assert int(ctx[0]) == len(rows[0][0])
+
+
+def test_captured_steps_replay():
+    """A captured decode step (rotation, append, attention with weights, eviction in place), replayed
+    with changed inputs and with eager work between, against the eager calls."""
+    from paper_2606_08382_amd.device import Rope
+    B, n_q, n_kv, d, T, cap = 2, 8, 2, 128, 16, 16 * 16
+    rope = Rope(d, 5e5)
+
+    def fresh():
+        layer = layer_of(B, n_q, n_kv, d, cap, 0, T)
+        k, v = kv(B, 100, n_kv, d)
+        layer.append(k.cuda(), v.cuda(), ints([0, 0]), n_new=ints([100, 70]))
+        return layer, layer.new_weights(), ints([100, 70])
+    x = torch.zeros(B, 1, n_q + 2 * n_kv, d, dtype=torch.bfloat16, device="cuda")
+    y = torch.zeros_like(x)
+    out = torch.zeros(B, 1, n_q, d, dtype=torch.bfloat16, device="cuda")
+    pos = ints([[0], [0]])
+
+    def step(layer, w, ctx):
+        rope(x[:, :, :n_q + n_kv], pos, out=y[:, :, :n_q + n_kv])
+        layer.append(y[:, :, n_q:n_q + n_kv], x[:, :, n_q + n_kv:], ctx)
+        ctx += 1
+        layer.attend(y[:, :, :n_q], ctx, weights=w, out=out)
+        layer.evict(w, ctx, 6, sink=1, recent=1)
+
+    captured, eager = fresh(), fresh()
+    for st in (fresh(),):                                    # (first launches outside the capture)
+        step(*st)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    start = [t.clone() for t in (captured[0].cache, captured[0].table, captured[1], captured[2])]
+    with torch.cuda.graph(graph):
+        step(*captured)
+    for t, s in zip((captured[0].cache, captured[0].table, captured[1], captured[2]), start):
+        t.copy_(s)
+    for i in range(40):
+        x.copy_(rand(B, 1, n_q + 2 * n_kv, d, seed=i, dtype=torch.bfloat16))
+        pos.fill_(500 + i)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = out.clone()
+        step(*eager)
+        torch.cuda.synchronize()
+        assert torch.equal(got, out), i
+        assert torch.equal(captured[1], eager[1]) and torch.equal(captured[2], eager[2]), i
+        assert torch.equal(captured[0].table, eager[0].table), i
+
+
+def test_layers_refuse_other_arrays():
+    from paper_2606_08382_amd.device import Rope
+    layer = layer_of(2, 4, 2, 64, 64, T=16)
+    ctx = ints([3, 3])
+    bf = dict(dtype=torch.bfloat16, device="cuda")
+    q = torch.zeros(2, 1, 4, 64, **bf)
+    kx = torch.zeros(2, 3, 2, 64, **bf)
+    for bad in (q.cpu(), q.half(), q[:1], q[..., :32], q.float(),
+                torch.zeros(2, 1, 4, 128, **bf)[..., ::2]):
+        with pytest.raises((ValueError, TypeError)):
+            layer.attend(bad, ctx)
+    for bad in (ctx.cpu(), ctx.long(), ctx[:1], ints([1, 2, 3, 4])[::2]):
+        for call in (lambda: layer.attend(q, bad), lambda: layer.append(kx, kx, bad),
+                     lambda: layer.append(kx, kx, ctx, n_new=bad),
+                     lambda: layer.attend(q, ctx, q_len=bad),
+                     lambda: layer.evict(layer.new_weights(), bad, 1)):
+            with pytest.raises((ValueError, TypeError)):
+                call()
+    with pytest.raises(ValueError):
+        layer.append(kx, kx[:, :2], ctx)
+    with pytest.raises((ValueError, TypeError)):
+        layer.attend(q, ctx, weights=layer.new_weights()[:, :1])
+    with pytest.raises(S.StarkvError):
+        layer.attend(q, ctx, ws=torch.empty(16, dtype=torch.uint8, device="cuda"))
+    with pytest.raises(ValueError):
+        Rope(64, 1e4)(q, ints([[1, 2], [3, 4]]))
