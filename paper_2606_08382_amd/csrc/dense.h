@@ -78,11 +78,11 @@ struct DenseAttnParams {
   const int32_t* q_len;
   const int32_t* ctx_len;
   float* weights;
-  float* part_o;                                // [item][H_kv][rows][d], normalized
-  Pair* part_ml;                            // [item][H_kv][rows]: (reference, sum)
+  float* part_o;                                // [slot][H_kv][rows][d], normalized
+  Pair* part_ml;                            // [slot][H_kv][rows]: (reference, sum)
   Pair* sub;                                // [B*H_kv][subtile][rows]: (sum, reference)
   int32_t n_q, group, rows;                     // rows = n_q * group
-  int32_t max_ctx, items, sub_per_head;
+  int32_t max_ctx, ranges, sub_per_head;
   int32_t q_wide;
   float scale_log2;                             // softmax scale * log2(e)
 };

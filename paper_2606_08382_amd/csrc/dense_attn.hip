@@ -36,20 +36,36 @@ typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u2 __attribute__((ext_vector_type(2)));
 
 constexpr int kWavesA = 4;
-constexpr int kUnit = 32 * kWavesA;         // tokens of a workgroup's round: granule of splits
+constexpr int kUnit = 32 * kWavesA;         // tokens of a workgroup's round: granule of ranges
 constexpr float kBelow = 6.0f;              // reference: largest score - kBelow (log2)
 constexpr float kAbove = 14.0f;             // scores may pass the reference by this much
 constexpr float kTinyScale = 0x1p-100f;     // smallest reference of the value scales
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
-__device__ __forceinline__ float quad_max(float v) {    // over the four lanes of a column
-  v = fmaxf(v, __shfl_xor(v, 16));
-  return fmaxf(v, __shfl_xor(v, 32));
+// Reductions over the four lanes of a column (lanes 16 and 32 apart), in all of them: a register
+// swapped with a copy of itself holds the even and the odd rows, or halves, of the wave.
+__device__ __forceinline__ void swap16(float v, float* a, float* b) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  *a = __uint_as_float(r[0]);
+  *b = __uint_as_float(r[1]);
+}
+__device__ __forceinline__ void swap32(float v, float* a, float* b) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  *a = __uint_as_float(r[0]);
+  *b = __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float quad_max(float v) {
+  float a, b;
+  swap16(v, &a, &b);
+  swap32(fmaxf(a, b), &a, &b);
+  return fmaxf(a, b);
 }
 __device__ __forceinline__ float quad_sum(float v) {
-  v += __shfl_xor(v, 16);
-  return v + __shfl_xor(v, 32);
+  float a, b;
+  swap16(v, &a, &b);
+  swap32(a + b, &a, &b);
+  return a + b;
 }
 
 // Four codes of a dword as fp16.
@@ -86,75 +102,66 @@ __device__ __forceinline__ float from16(uint32_t u, int bf16) {
 }
 
 // ---- work plan ----------------------------------------------------------------------
-// Splits of all sequences as one list of work items of equal length: S units of kUnit tokens
-// with S the smallest for which sum_b ceil(u_b / S) <= items, bounded by
-// S = ceil(sum u_b / (items - B)) (each sequence adds at most one part item).  items == B: one
-// item per sequence.  Every wave derives it from the lengths, so nothing is planned on the host
-// and a captured call serves any lengths.
+// The sequences' tokens, in units of kUnit, lie end to end; range w of p.ranges takes the units
+// [w R, (w + 1) R), R = ceil(all units / ranges), and with them the end of one sequence and the
+// start of the next: ranges are equal however ragged the lengths are.  The part of sequence b in
+// range w is slot w + b of the partials (one of the two grows from part to part), at most
+// ranges + B of them.  Every wave derives this from the lengths, so nothing is planned on the
+// host and a captured call serves any lengths.
 __device__ __forceinline__ int clamp_ctx(const DenseAttnParams& p, int b) {
   return min(max(p.ctx_len[b], 0), p.max_ctx);
 }
+__device__ __forceinline__ int units_of(int ctx) { return (ctx + kUnit - 1) / kUnit; }
 
-__device__ __forceinline__ int plan_units(const DenseAttnParams& p, int lane) {
-  const int B = p.c.batch;
-  if (p.items == B) return 1 << 30;
-  int sum = 0;                                   // < 2^31: B <= 32767, u <= 4096
-  for (int b = lane; b < B; b += 64) sum += (clamp_ctx(p, b) + kUnit - 1) / kUnit;
+// Units of a range.
+__device__ __forceinline__ int range_units(const DenseAttnParams& p, int lane) {
+  int sum = 0;                                   // < 2^31: B <= 32767, 4096 units each at most
+  for (int b = lane; b < p.c.batch; b += 64) sum += units_of(clamp_ctx(p, b));
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) sum += __shfl_xor(sum, o);
-  const int room = p.items - B;
-  return max((sum + room - 1) / room, 1);
+  return max((sum + p.ranges - 1) / p.ranges, 1);
 }
 
-struct Item {
-  int b, ctx, t0, t1;                            // tokens [t0, t1) of the sequence
+// The sequence that holds unit `at`, its length and its first unit; false past the last.
+struct Place {
+  int b, ctx, start;
 };
-__device__ __forceinline__ bool find_item(const DenseAttnParams& p, int S, int lane, Item* it) {
-  int want = blockIdx.x;
+__device__ __forceinline__ bool find_unit(const DenseAttnParams& p, int at, int lane, Place* pl) {
+  int before = 0;
   for (int b0 = 0; b0 < p.c.batch; b0 += 64) {
     const int b = b0 + lane;
     const int ctx = b < p.c.batch ? clamp_ctx(p, b) : 0;
-    const int u = (ctx + kUnit - 1) / kUnit;
-    const int cnt = S >= (1 << 30) ? (u > 0) : (u + S - 1) / S;
-    int incl = cnt;
+    const int u = units_of(ctx);
+    int incl = u;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
       const int y = __shfl_up(incl, o);
       if (lane >= o) incl += y;
     }
-    const uint64_t hit = __ballot(incl > want);
+    incl += before;
+    const uint64_t hit = __ballot(incl > at);
     if (hit) {
       const int l = (int)__builtin_ctzll(hit);
-      const int split = want - (__builtin_amdgcn_readlane(incl, l) - __builtin_amdgcn_readlane(cnt, l));
-      it->b = b0 + l;
-      it->ctx = __builtin_amdgcn_readlane(ctx, l);
-      const int64_t len = (int64_t)S * kUnit;
-      it->t0 = S >= (1 << 30) ? 0 : (int)(split * len);
-      it->t1 = (int)min((int64_t)it->t0 + len, (int64_t)it->ctx);
+      pl->b = b0 + l;
+      pl->ctx = __builtin_amdgcn_readlane(ctx, l);
+      pl->start = __builtin_amdgcn_readlane(incl, l) - units_of(pl->ctx);
       return true;
     }
-    want -= __builtin_amdgcn_readlane(incl, 63);
+    before = __builtin_amdgcn_readlane(incl, 63);
   }
   return false;
 }
-// First item and number of items of sequence b.
-__device__ __forceinline__ void items_of(const DenseAttnParams& p, int S, int b, int lane, int* first,
+// First slot and number of slots of sequence b.
+__device__ __forceinline__ void slots_of(const DenseAttnParams& p, int b, int lane, int* first,
                                          int* count) {
-  int before = 0, own = 0;
-  for (int b0 = 0; b0 <= b; b0 += 64) {
-    const int x = b0 + lane;
-    const int u = x <= b ? (clamp_ctx(p, x) + kUnit - 1) / kUnit : 0;
-    const int cnt = S >= (1 << 30) ? (u > 0) : (u + S - 1) / S;
-    before += x < b ? cnt : 0;
-    own += x == b ? cnt : 0;
-  }
+  const int R = range_units(p, lane);
+  int before = 0;
+  for (int x = lane; x < b; x += 64) before += units_of(clamp_ctx(p, x));
 #pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) {
-    before += __shfl_xor(before, o);
-    own += __shfl_xor(own, o);
-  }
-  *first = before;
-  *count = own;
+  for (int o = 32; o >= 1; o >>= 1) before += __shfl_xor(before, o);
+  const int u = units_of(clamp_ctx(p, b));
+  *first = before / R + b;
+  *count = u > 0 ? (before + u - 1) / R - before / R + 1 : 0;
 }
 
 // Tokens that query row r (query token r / group) of sequence b sees: at most ctx; 0: none;
@@ -164,6 +171,11 @@ __device__ __forceinline__ int row_limit(const DenseAttnParams& p, int b, int ct
   const int j = r / p.group;
   if (r >= p.rows || j >= q_len) return -1;
   return max(ctx - q_len + j + 1, 0);
+}
+
+__device__ __forceinline__ int fresh(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
 }
 
 // ---- split --------------------------------------------------------------------------
@@ -207,14 +219,27 @@ __device__ __forceinline__ void raise(State<D, RT>& s, const float* top, float s
 
 template <int D, bool E4M3, int RT, bool SUMS>
 __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void dense_split_kernel(const DenseAttnParams p) {
-  constexpr int N = D / 64, CT = D / 16;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int col = lane & 15, quad = lane >> 4;
+  constexpr int N = D / 64, CT = D / 16, NB = RT == 1 ? 3 : 2;
+  const int tid_lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = blockIdx.y, row0 = blockIdx.z * (16 * RT);
-  const int S = plan_units(p, lane);
-  Item it;
-  if (!find_item(p, S, lane, &it)) return;
+  const int R = range_units(p, tid_lane);
+  __shared__ float so[kWavesA][16][D + 4];
+  __shared__ float sm[kWavesA][RT * 16], sl[kWavesA][RT * 16];
   const int sh = p.c.shift, T = 1 << sh;
+  Place pl;
+  int at = blockIdx.x * R;
+  const int at_end = at + R;
+  if (!find_unit(p, at, tid_lane, &pl)) return;
+  for (;;) {                                       // the range's part of one sequence after another
+  // (a lane index that the compiler takes for new: addresses and masks are formed where they are
+  // used instead of being kept in registers over the whole range)
+  int lane = fresh(tid_lane);
+  int col = lane & 15, quad = lane >> 4;
+  struct { int b, ctx, t0, t1; } it;
+  it.b = pl.b;
+  it.ctx = pl.ctx;
+  it.t0 = (at - pl.start) * kUnit;
+  it.t1 = min((at_end - pl.start) * kUnit, pl.ctx);
   const int full = it.ctx & ~(T - 1);
   const int64_t head = (int64_t)it.b * p.c.n_kv + g;
 
@@ -325,7 +350,7 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void dense_split_kernel(const
   // ---- finished blocks
   const uint8_t* codes = p.c.codes;
   const int e8 = min(it.t1, full), tw = it.t0 + 32 * wave;
-  // (row tiles of early query tokens end before the sequence does; an item's sums are written
+  // (row tiles of early query tokens end before the sequence does; a part's sums are written
   // for all of its subtiles)
   const int stop = SUMS ? e8 : min(e8, (lim_hi + 15) & ~15);
   const int steps = stop > tw ? (stop - tw + kUnit - 1) / kUnit : 0;
@@ -350,9 +375,9 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void dense_split_kernel(const
       const uint8_t* kb = codes + (uint64_t)sub * (16 * D);
       const uint8_t* vb = codes + (uint64_t)(sub + v_sub) * (16 * D);
 #pragma unroll
-      for (int n = 0; n < N; ++n) x.k[a][n] = *reinterpret_cast<const u4*>(kb + n * 1024 + lane * 16);
+      for (int n = 0; n < N; ++n) x.k[a][n] = __builtin_nontemporal_load(reinterpret_cast<const u4*>(kb + n * 1024 + lane * 16));
 #pragma unroll
-      for (int n = 0; n < N; ++n) x.v[a][n] = *reinterpret_cast<const u4*>(vb + n * 1024 + lane * 16);
+      for (int n = 0; n < N; ++n) x.v[a][n] = __builtin_nontemporal_load(reinterpret_cast<const u4*>(vb + n * 1024 + lane * 16));
     }
   };
   auto compute = [&](const Tile<D>& x, int i) {
@@ -377,16 +402,17 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void dense_split_kernel(const
     softmax(sc, t, e8, x.sv, pr, t + 16 < e8);
     h8 ph[RT];
     const float f0 = x.sv[0] * s.vinv, f1 = x.sv[1] * s.vinv;
-    const bool masked = t + 32 > lim_lo || t + 32 > e8;
 #pragma unroll
     for (int r = 0; r < RT; ++r)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        float v = pr[r][e] * (e < 4 ? f0 : f1);
-        // an absent token's probability is zero whatever its block's scale
-        if (masked && pr[r][e] == 0.0f) v = 0.0f;
-        ph[r][e] = (_Float16)v;
-      }
+      for (int e = 0; e < 8; ++e) ph[r][e] = (_Float16)(pr[r][e] * (e < 4 ? f0 : f1));
+    if (t + 32 > lim_lo || t + 32 > e8) {
+      // an absent token's probability is zero whatever its block's scale
+#pragma unroll
+      for (int r = 0; r < RT; ++r)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) ph[r][e] = pr[r][e] == 0.0f ? (_Float16)0.0f : ph[r][e];
+    }
 #pragma unroll
     for (int n = 0; n < N; ++n)
 #pragma unroll
@@ -397,25 +423,33 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void dense_split_kernel(const
       }
   };
   if (steps > 0) {
-    // a step's codes are loaded one step ahead, past the last one the last again (cached); the
-    // entries of the next 32 steps while these 32 run
+    // A step's codes are loaded NB - 1 steps ahead, past the last one the last again (cached); the
+    // entries of the next 32 steps while these 32 run.
     Entry now = entries(0), next = entries(32);
-    Tile<D> a, c;
-    load(a, now, 0);
-    for (int i = 0; i < steps; i += 2) {
-      load(c, now, min(i + 1, steps - 1));
-      compute(a, i);
-      if (((i + 2) & 31) == 0) {
+    Tile<D> x[NB];
+    auto fetch = [&](Tile<D>& y, int i) {
+      if (i > 0 && (i & 31) == 0) {
         now = next;
-        next = entries(i + 34);
+        next = entries(i + 32);
       }
-      load(a, now, min(i + 2, steps - 1));
-      if (i + 1 < steps) compute(c, i + 1);
+      load(y, now, min(i, steps - 1));
+    };
+#pragma unroll
+    for (int u = 0; u < NB - 1; ++u) fetch(x[u], u);
+    for (int i = 0; i < steps; i += NB) {
+#pragma unroll
+      for (int u = 0; u < NB; ++u) {
+        fetch(x[(u + NB - 1) % NB], i + u + NB - 1);
+        if (i + u < steps) compute(x[u], i + u);
+      }
     }
   }
 
   // ---- the unfinished block, from its 16-bit rows
   if (full < it.t1 && (SUMS || lim_hi > full)) {
+    lane = fresh(tid_lane);
+    col = lane & 15;
+    quad = lane >> 4;
     const uint16_t* kt = p.c.tails + head * 2 * (2 * T * D);
     const uint16_t* vt = kt + 2 * T * D;
     for (int t = full + 32 * wave; t < it.ctx; t += kUnit) {
@@ -503,9 +537,10 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void dense_split_kernel(const
     }
   }
 
-  // ---- the waves' states merged, normalized and written as the item's partial
-  __shared__ float so[kWavesA][16][D + 4];
-  __shared__ float sm[kWavesA][RT * 16], sl[kWavesA][RT * 16];
+  lane = fresh(tid_lane);
+  col = lane & 15;
+  quad = lane >> 4;
+  // ---- the waves' states merged, normalized and written as the part's partial
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
     const float l = quad_sum(s.l[r]);
@@ -515,7 +550,7 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void dense_split_kernel(const
     }
   }
   __syncthreads();
-  const int64_t slot0 = ((int64_t)blockIdx.x * p.c.n_kv + g) * p.rows + row0;
+  const int64_t slot0 = ((int64_t)(blockIdx.x + it.b) * p.c.n_kv + g) * p.rows + row0;
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
     float M = -__builtin_inff();
@@ -551,11 +586,14 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void dense_split_kernel(const
     }
     __syncthreads();
   }
+  at = pl.start + units_of(pl.ctx);
+  if (at >= at_end || !find_unit(p, at, tid_lane, &pl)) return;
+  }
 }
 
 // ---- combine ------------------------------------------------------------------------
-// A workgroup per (row, KV head, sequence): items' normalized outputs weighted by their
-// softmax sums.  Four waves take every fourth item.
+// A workgroup per (row, KV head, sequence): the parts' normalized outputs weighted by their
+// softmax sums.  Four waves take every fourth part.
 template <int D>
 __global__ __launch_bounds__(256) void dense_combine_kernel(const DenseAttnParams p) {
   constexpr int C = D / 64;
@@ -565,10 +603,9 @@ __global__ __launch_bounds__(256) void dense_combine_kernel(const DenseAttnParam
   const int ctx = clamp_ctx(p, b);
   const int lim = row_limit(p, b, ctx, row);
   if (lim < 0) return;
-  const int S = plan_units(p, lane);
   int first, count;
-  items_of(p, S, b, lane, &first, &count);
-  // this wave's items: its largest reference and its sum
+  slots_of(p, b, lane, &first, &count);
+  // this wave's parts: their largest reference and sum
   float m = -__builtin_inff(), l = 0.0f, o[C] = {};
   for (int i = wave; i < count; i += 4) {
     const int64_t slot = ((int64_t)(first + i) * p.c.n_kv + g) * p.rows + row;
@@ -620,9 +657,8 @@ __global__ __launch_bounds__(256) void dense_weights_kernel(const DenseAttnParam
   const int per = 1 << (p.c.shift - 4);
   const int subs = (ctx + 15) >> 4;
   if (blockIdx.x * 256 * per >= subs) return;
-  const int S = plan_units(p, lane);
   int first, count;
-  items_of(p, S, b, lane, &first, &count);
+  slots_of(p, b, lane, &first, &count);
   for (int row = threadIdx.x; row < p.rows; row += 256) {
     float M = -__builtin_inff(), L = 0.0f;
     if (row_limit(p, b, ctx, row) > 0) {
@@ -653,7 +689,7 @@ __global__ __launch_bounds__(256) void dense_weights_kernel(const DenseAttnParam
 
 template <int D, bool E4M3, int RT>
 void launch_split(const DenseAttnParams& p, hipStream_t st) {
-  const dim3 grid(p.items, p.c.n_kv, (p.rows + 16 * RT - 1) / (16 * RT));
+  const dim3 grid(p.ranges, p.c.n_kv, (p.rows + 16 * RT - 1) / (16 * RT));
   if (p.weights) hipLaunchKernelGGL((dense_split_kernel<D, E4M3, RT, true>), grid, dim3(256), 0, st, p);
   else hipLaunchKernelGGL((dense_split_kernel<D, E4M3, RT, false>), grid, dim3(256), 0, st, p);
 }

@@ -353,16 +353,16 @@ starkv_status starkv_dense_read(const starkv_dense_plan* P, const void* cache,
 
 // ----------------------------------------------------------------------------- attention
 
-// Work items of a split pass over `rows` query rows per KV head: one per sequence, and as many
-// more as bring the launch to kSplitTarget workgroups.
-static int64_t split_items(const starkv_dense_plan* P, int64_t rows) {
-  const int64_t per_item = P->cfg.n_kv_heads * ((rows + 63) / 64);
-  const int64_t B = P->cfg.batch;
-  return B * per_item >= kSplitTarget ? B : B + (kSplitTarget + per_item - 1) / per_item;
+// Ranges of a split pass over `rows` query rows per KV head: they bring the launch to kSplitTarget
+// workgroups.
+static int64_t split_ranges(const starkv_dense_plan* P, int64_t rows) {
+  const int64_t per_range = P->cfg.n_kv_heads * ((rows + 63) / 64);
+  return (kSplitTarget + per_range - 1) / per_range;
 }
 
 struct DenseWorkspace {
-  int64_t items, ml, sub, total;      // offsets in bytes; the outputs' partials come first
+  int64_t ranges;
+  int64_t ml, sub, total;             // offsets in bytes; the outputs' partials come first
   int32_t sub_per_head;
 };
 static DenseWorkspace workspace_of(const starkv_dense_plan* P, int32_t n_q, int32_t max_ctx,
@@ -370,8 +370,8 @@ static DenseWorkspace workspace_of(const starkv_dense_plan* P, int32_t n_q, int3
   DenseWorkspace w;
   const starkv_dense_config& c = P->cfg;
   const int64_t rows = (int64_t)n_q * (c.n_q_heads / c.n_kv_heads);
-  w.items = split_items(P, rows);
-  const int64_t slots = w.items * c.n_kv_heads * rows;
+  w.ranges = split_ranges(P, rows);
+  const int64_t slots = (w.ranges + c.batch) * c.n_kv_heads * rows;
   w.ml = align256(slots * c.head_dim * 4);
   w.sub = w.ml + align256(slots * 8);
   w.sub_per_head = (max_ctx + 15) / 16;
@@ -382,7 +382,7 @@ static DenseWorkspace workspace_of(const starkv_dense_plan* P, int32_t n_q, int3
 size_t starkv_dense_workspace_bytes(const starkv_dense_plan* P, int32_t n_q, int32_t max_ctx,
                                     int32_t with_weights) {
   if (!P || n_q < 1 || max_ctx < 1) return 0;
-  // Fewer query tokens may take more items: the largest need lies at n_q or just before a step
+  // Fewer query tokens may take more ranges: the largest need lies at n_q or just before a step
   // of the row tiles.
   const int G = P->cfg.n_q_heads / P->cfg.n_kv_heads;
   const int gather = with_weights ? std::min(n_q, std::max(64 / G, 1)) : 0;
@@ -424,7 +424,6 @@ starkv_status starkv_dense_attn(const starkv_dense_plan* P, const void* cache, c
   if (!ws || ws_bytes < (size_t)w.total)
     return fail_with(STARKV_ERR_WORKSPACE, "attention workspace %zu bytes < %lld", ws_bytes, (long long)w.total);
   if (misaligned(ws, 256)) return fail_with(STARKV_ERR_ALIGNMENT, "ws not 256-byte aligned");
-  if (w.items > 0x7fffffff) return fail_with(STARKV_ERR_UNSUPPORTED, "too many work items");
   DenseAttnParams p;
   std::memset(&p, 0, sizeof(p));
   p.c = cache_of(P, cache);
@@ -447,7 +446,7 @@ starkv_status starkv_dense_attn(const starkv_dense_plan* P, const void* cache, c
   p.group = G;
   p.rows = n_q * G;
   p.max_ctx = max_ctx;
-  p.items = (int32_t)w.items;
+  p.ranges = (int32_t)w.ranges;
   p.sub_per_head = w.sub_per_head;
   p.q_wide = rows_wide(q, a, 2);
   p.scale_log2 = (float)(P->scale * 1.4426950408889634);
