@@ -113,55 +113,76 @@ __device__ __forceinline__ int clamp_ctx(const DenseAttnParams& p, int b) {
 }
 __device__ __forceinline__ int units_of(int ctx) { return (ctx + kUnit - 1) / kUnit; }
 
-// Units of a range.
-__device__ __forceinline__ int range_units(const DenseAttnParams& p, int lane) {
-  int sum = 0;                                   // < 2^31: B <= 32767, 4096 units each at most
-  for (int b = lane; b < p.c.batch; b += 64) sum += units_of(clamp_ctx(p, b));
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) sum += __shfl_xor(sum, o);
-  return max((sum + p.ranges - 1) / p.ranges, 1);
+// Inclusive sum over the wave's lanes (row shifts, then the rows' ends broadcast).
+__device__ __forceinline__ int wave_scan(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);    // row_shr:1
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);   // row_bcast:15
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);   // row_bcast:31
+  return v;
+}
+
+// Lane l: length of sequence l of the first 64 and the units up to its end.
+struct Lens {
+  int ctx, incl;
+};
+__device__ __forceinline__ Lens first_lens(const DenseAttnParams& p, int lane) {
+  const int ctx = lane < p.c.batch ? clamp_ctx(p, lane) : 0;
+  return {ctx, wave_scan(units_of(ctx))};
+}
+
+// Units of a range (all of them: < 2^31, with B <= 32767 and 4096 units each at most).
+__device__ __forceinline__ int range_units(const DenseAttnParams& p, const Lens& ls, int lane) {
+  int sum = __builtin_amdgcn_readlane(ls.incl, 63);
+  for (int b0 = 64; b0 < p.c.batch; b0 += 64) {
+    const int b = b0 + lane;
+    sum += __builtin_amdgcn_readlane(wave_scan(b < p.c.batch ? units_of(clamp_ctx(p, b)) : 0), 63);
+  }
+  return max((int)(((uint32_t)sum + (uint32_t)p.ranges - 1) / (uint32_t)p.ranges), 1);
 }
 
 // The sequence that holds unit `at`, its length and its first unit; false past the last.
 struct Place {
   int b, ctx, start;
 };
-__device__ __forceinline__ bool find_unit(const DenseAttnParams& p, int at, int lane, Place* pl) {
-  int before = 0;
-  for (int b0 = 0; b0 < p.c.batch; b0 += 64) {
-    const int b = b0 + lane;
-    const int ctx = b < p.c.batch ? clamp_ctx(p, b) : 0;
-    const int u = units_of(ctx);
-    int incl = u;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int y = __shfl_up(incl, o);
-      if (lane >= o) incl += y;
-    }
-    incl += before;
-    const uint64_t hit = __ballot(incl > at);
+__device__ __forceinline__ bool find_unit(const DenseAttnParams& p, const Lens& ls, int at, int lane,
+                                          Place* pl) {
+  Lens x = ls;
+  for (int b0 = 0;;) {
+    const uint64_t hit = __ballot(x.incl > at);
     if (hit) {
       const int l = (int)__builtin_ctzll(hit);
       pl->b = b0 + l;
-      pl->ctx = __builtin_amdgcn_readlane(ctx, l);
-      pl->start = __builtin_amdgcn_readlane(incl, l) - units_of(pl->ctx);
+      pl->ctx = __builtin_amdgcn_readlane(x.ctx, l);
+      pl->start = __builtin_amdgcn_readlane(x.incl, l) - units_of(pl->ctx);
       return true;
     }
-    before = __builtin_amdgcn_readlane(incl, 63);
+    b0 += 64;
+    if (b0 >= p.c.batch) return false;
+    const int b = b0 + lane, before = __builtin_amdgcn_readlane(x.incl, 63);
+    x.ctx = b < p.c.batch ? clamp_ctx(p, b) : 0;
+    x.incl = before + wave_scan(units_of(x.ctx));
   }
-  return false;
 }
-// First slot and number of slots of sequence b.
+// First slot and number of slots of sequence b, and its length.
 __device__ __forceinline__ void slots_of(const DenseAttnParams& p, int b, int lane, int* first,
-                                         int* count) {
-  const int R = range_units(p, lane);
+                                         int* count, int* ctx) {
+  const Lens ls = first_lens(p, lane);
+  const uint32_t R = range_units(p, ls, lane);
+  Lens x = ls;
   int before = 0;
-  for (int x = lane; x < b; x += 64) before += units_of(clamp_ctx(p, x));
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) before += __shfl_xor(before, o);
-  const int u = units_of(clamp_ctx(p, b));
-  *first = before / R + b;
-  *count = u > 0 ? (before + u - 1) / R - before / R + 1 : 0;
+  for (int b0 = 64; b0 <= b; b0 += 64) {
+    before += __builtin_amdgcn_readlane(x.incl, 63);
+    x.ctx = b0 + lane < p.c.batch ? clamp_ctx(p, b0 + lane) : 0;
+    x.incl = wave_scan(units_of(x.ctx));
+  }
+  *ctx = __builtin_amdgcn_readlane(x.ctx, b & 63);
+  const uint32_t u = units_of(*ctx);
+  const uint32_t start = before + __builtin_amdgcn_readlane(x.incl, b & 63) - u;
+  *first = start / R + b;
+  *count = u > 0 ? (start + u - 1) / R - start / R + 1 : 0;
 }
 
 // Tokens that query row r (query token r / group) of sequence b sees: at most ctx; 0: none;
@@ -222,14 +243,15 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void dense_split_kernel(const
   constexpr int N = D / 64, CT = D / 16, NB = RT == 1 ? 3 : 2;
   const int tid_lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = blockIdx.y, row0 = blockIdx.z * (16 * RT);
-  const int R = range_units(p, tid_lane);
+  const Lens lens = first_lens(p, tid_lane);
+  const int R = range_units(p, lens, tid_lane);
   __shared__ float so[kWavesA][16][D + 4];
   __shared__ float sm[kWavesA][RT * 16], sl[kWavesA][RT * 16];
   const int sh = p.c.shift, T = 1 << sh;
   Place pl;
   int at = blockIdx.x * R;
   const int at_end = at + R;
-  if (!find_unit(p, at, tid_lane, &pl)) return;
+  if (!find_unit(p, lens, at, tid_lane, &pl)) return;
   for (;;) {                                       // the range's part of one sequence after another
   // (a lane index that the compiler takes for new: addresses and masks are formed where they are
   // used instead of being kept in registers over the whole range)
@@ -239,15 +261,26 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void dense_split_kernel(const
   it.b = pl.b;
   it.ctx = pl.ctx;
   it.t0 = (at - pl.start) * kUnit;
-  it.t1 = min((at_end - pl.start) * kUnit, pl.ctx);
+  it.t1 = min(min(at_end - pl.start, units_of(pl.ctx)) * kUnit, pl.ctx);
   const int full = it.ctx & ~(T - 1);
   const int64_t head = (int64_t)it.b * p.c.n_kv + g;
+  const int e8 = min(it.t1, full), tw = it.t0 + 32 * wave;   // the wave's finished blocks
+
+  // The chains of loads that a part begins with overlap: the table entries of the first 64 steps
+  // (a subtile per lane and 32 steps), the queries, then the entries' scales and codes.
+  const int32_t* table = p.c.table + head * p.c.blocks_per_head;
+  auto entry_token = [&](int i0) {
+    return max(min(tw + (i0 + (lane >> 1)) * kUnit + (lane & 1) * 16, e8 - 16), 0);
+  };
+  const int entry0 = table[entry_token(0) >> sh], entry1 = table[entry_token(32) >> sh];
 
   // queries: row r of the tile in column `col`, channels i*64 + quad*16 + h*8 + e
   h8 q[RT][2 * N];
   float qs[RT];
   int lim[RT];
   int lim_lo = 0x7fffffff, lim_hi = 0;
+  union Raw { u4 v; uint16_t h[8]; };
+  Raw raw[RT][2 * N];
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
     const int row = row0 + r * 16 + col;
@@ -257,31 +290,19 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void dense_split_kernel(const
     lim_hi = max(lim_hi, lm);
     const int jq = row / p.group, iq = row % p.group;
     const uint16_t* src = p.q + it.b * p.qs_b + jq * p.qs_t + (g * p.group + iq) * p.qs_h;
-    union { u4 v; uint16_t h[8]; } raw[2 * N];
-    float top = 0.0f;
 #pragma unroll
     for (int i = 0; i < 2 * N; ++i) {
       const int ch = (i >> 1) * 64 + quad * 16 + (i & 1) * 8;
-      raw[i].v = (u4){0, 0, 0, 0};
+      raw[r][i].v = (u4){0, 0, 0, 0};
       if (lm >= 0) {
         if (p.q_wide) {
-          raw[i].v = *reinterpret_cast<const u4*>(src + ch);
+          raw[r][i].v = *reinterpret_cast<const u4*>(src + ch);
         } else {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) raw[i].h[e] = src[ch + e];
+          for (int e = 0; e < 8; ++e) raw[r][i].h[e] = src[ch + e];
         }
       }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(from16(raw[i].h[e], p.c.bf16)));
     }
-    top = quad_max(top);
-    const int ex = top > 0.0f && top < __builtin_inff() ? 8 - __builtin_amdgcn_frexp_expf(top) : 0;
-#pragma unroll
-    for (int i = 0; i < 2 * N; ++i)
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        q[r][i][e] = (_Float16)__builtin_amdgcn_ldexpf(from16(raw[i].h[e], p.c.bf16), ex);
-    qs[r] = __builtin_amdgcn_ldexpf(p.scale_log2, -ex);
   }
 #pragma unroll
   for (int o = 8; o >= 1; o >>= 1) {
@@ -290,6 +311,72 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void dense_split_kernel(const
   }
   lim_lo = __builtin_amdgcn_readfirstlane(lim_lo);
   lim_hi = __builtin_amdgcn_readfirstlane(lim_hi);
+
+  // row tiles of early query tokens end before the sequence does; a part's sums are written for
+  // all of its subtiles
+  const int stop = SUMS ? e8 : min(e8, (lim_hi + 15) & ~15);
+  const int steps = stop > tw ? (stop - tw + kUnit - 1) / kUnit : 0;
+  struct Entry { uint32_t sub; float sk, sv; };
+  auto entry_of = [&](int e, int i0) {
+    const int t = entry_token(i0);
+    e = min(max(e, 0), p.c.n_blocks - 1);
+    const Pair sc = p.c.scales[e];
+    return Entry{((uint32_t)e << (sh - 3)) + ((uint32_t)(t & (T - 1)) >> 4), sc.x, sc.y};
+  };
+  const uint32_t v_sub = (uint32_t)T >> 4;          // from a key subtile to its value subtile
+  auto load = [&](Tile<D>& x, const Entry& en, int i) {
+#pragma unroll
+    for (int a = 0; a < 2; ++a) {
+      const int l = 2 * (i & 31) + a;
+      const uint32_t sub = __builtin_amdgcn_readlane(en.sub, l);
+      x.sk[a] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(en.sk), l));
+      x.sv[a] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(en.sv), l));
+      const uint8_t* kb = p.c.codes + (uint64_t)sub * (16 * D) + lane * 16;
+      const uint8_t* vb = p.c.codes + (uint64_t)(sub + v_sub) * (16 * D) + lane * 16;
+      // (streaming: a code is read once a step; 5.8 TB/s with plain loads, 6.7 with these)
+#pragma unroll
+      for (int n = 0; n < N; ++n)
+        x.k[a][n] = __builtin_nontemporal_load(reinterpret_cast<const u4*>(kb + n * 1024));
+#pragma unroll
+      for (int n = 0; n < N; ++n)
+        x.v[a][n] = __builtin_nontemporal_load(reinterpret_cast<const u4*>(vb + n * 1024));
+    }
+  };
+  // A step's codes are loaded NB - 1 steps ahead, past the last one the last again; the entries of
+  // the next 32 steps while these 32 run.
+  Entry now, next;
+  Tile<D> x[NB];
+  auto fetch = [&](Tile<D>& y, int i) {
+    if (i > 0 && (i & 31) == 0) {
+      now = next;
+      next = entry_of(table[entry_token(i + 32) >> sh], i + 32);
+    }
+    load(y, now, min(i, steps - 1));
+  };
+  if (steps > 0) {
+    now = entry_of(entry0, 0);
+    next = entry_of(entry1, 32);
+#pragma unroll
+    for (int u = 0; u < NB - 1; ++u) fetch(x[u], u);
+  }
+
+  // queries as fp16, scaled by a power of two per row
+#pragma unroll
+  for (int r = 0; r < RT; ++r) {
+    float top = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 2 * N; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(from16(raw[r][i].h[e], p.c.bf16)));
+    top = quad_max(top);
+    const int ex = top > 0.0f && top < __builtin_inff() ? 8 - __builtin_amdgcn_frexp_expf(top) : 0;
+#pragma unroll
+    for (int i = 0; i < 2 * N; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        q[r][i][e] = (_Float16)__builtin_amdgcn_ldexpf(from16(raw[r][i].h[e], p.c.bf16), ex);
+    qs[r] = __builtin_amdgcn_ldexpf(p.scale_log2, -ex);
+  }
 
   State<D, RT> s;
 #pragma unroll
@@ -348,39 +435,7 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void dense_split_kernel(const
   };
 
   // ---- finished blocks
-  const uint8_t* codes = p.c.codes;
-  const int e8 = min(it.t1, full), tw = it.t0 + 32 * wave;
-  // (row tiles of early query tokens end before the sequence does; a part's sums are written
-  // for all of its subtiles)
-  const int stop = SUMS ? e8 : min(e8, (lim_hi + 15) & ~15);
-  const int steps = stop > tw ? (stop - tw + kUnit - 1) / kUnit : 0;
-  // table entries and scales of 32 steps, a subtile per lane
-  struct Entry { uint32_t sub; float sk, sv; };
-  auto entries = [&](int i0) {
-    int t = tw + (i0 + (lane >> 1)) * kUnit + (lane & 1) * 16;
-    t = min(t, e8 - 16);
-    int e = p.c.table[head * p.c.blocks_per_head + (t >> sh)];
-    e = min(max(e, 0), p.c.n_blocks - 1);
-    const Pair sc = p.c.scales[e];
-    return Entry{((uint32_t)e << (sh - 3)) + ((uint32_t)(t & (T - 1)) >> 4), sc.x, sc.y};
-  };
-  const uint32_t v_sub = (uint32_t)T >> 4;          // from a key subtile to its value subtile
-  auto load = [&](Tile<D>& x, const Entry& en, int i) {
-#pragma unroll
-    for (int a = 0; a < 2; ++a) {
-      const int l = 2 * (i & 31) + a;
-      const uint32_t sub = __builtin_amdgcn_readlane(en.sub, l);
-      x.sk[a] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(en.sk), l));
-      x.sv[a] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(en.sv), l));
-      const uint8_t* kb = codes + (uint64_t)sub * (16 * D);
-      const uint8_t* vb = codes + (uint64_t)(sub + v_sub) * (16 * D);
-#pragma unroll
-      for (int n = 0; n < N; ++n) x.k[a][n] = __builtin_nontemporal_load(reinterpret_cast<const u4*>(kb + n * 1024 + lane * 16));
-#pragma unroll
-      for (int n = 0; n < N; ++n) x.v[a][n] = __builtin_nontemporal_load(reinterpret_cast<const u4*>(vb + n * 1024 + lane * 16));
-    }
-  };
-  auto compute = [&](const Tile<D>& x, int i) {
+  auto compute = [&](const Tile<D>& y, int i) {
     const int t = tw + i * kUnit;
     f4 sc[RT][2];
 #pragma unroll
@@ -391,17 +446,17 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void dense_split_kernel(const
       for (int n = 0; n < N; ++n)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const h8 k = code8<E4M3>(x.k[a][n][2 * h], x.k[a][n][2 * h + 1]);
+          const h8 k = code8<E4M3>(y.k[a][n][2 * h], y.k[a][n][2 * h + 1]);
 #pragma unroll
           for (int r = 0; r < RT; ++r) sc[r][a] = mfma_f16(k, q[r][2 * n + h], sc[r][a]);
         }
 #pragma unroll
-      for (int r = 0; r < RT; ++r) sc[r][a] *= x.sk[a] * qs[r];
+      for (int r = 0; r < RT; ++r) sc[r][a] *= y.sk[a] * qs[r];
     }
     float pr[RT][8];
-    softmax(sc, t, e8, x.sv, pr, t + 16 < e8);
+    softmax(sc, t, e8, y.sv, pr, t + 16 < e8);
     h8 ph[RT];
-    const float f0 = x.sv[0] * s.vinv, f1 = x.sv[1] * s.vinv;
+    const float f0 = y.sv[0] * s.vinv, f1 = y.sv[1] * s.vinv;
 #pragma unroll
     for (int r = 0; r < RT; ++r)
 #pragma unroll
@@ -417,25 +472,12 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void dense_split_kernel(const
     for (int n = 0; n < N; ++n)
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const h8 v = code8<E4M3>(x.v[0][n][j], x.v[1][n][j]);
+        const h8 v = code8<E4M3>(y.v[0][n][j], y.v[1][n][j]);
 #pragma unroll
         for (int r = 0; r < RT; ++r) s.o[r][n * 4 + j] = mfma_f16(v, ph[r], s.o[r][n * 4 + j]);
       }
   };
   if (steps > 0) {
-    // A step's codes are loaded NB - 1 steps ahead, past the last one the last again (cached); the
-    // entries of the next 32 steps while these 32 run.
-    Entry now = entries(0), next = entries(32);
-    Tile<D> x[NB];
-    auto fetch = [&](Tile<D>& y, int i) {
-      if (i > 0 && (i & 31) == 0) {
-        now = next;
-        next = entries(i + 32);
-      }
-      load(y, now, min(i, steps - 1));
-    };
-#pragma unroll
-    for (int u = 0; u < NB - 1; ++u) fetch(x[u], u);
     for (int i = 0; i < steps; i += NB) {
 #pragma unroll
       for (int u = 0; u < NB; ++u) {
@@ -587,104 +629,114 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void dense_split_kernel(const
     __syncthreads();
   }
   at = pl.start + units_of(pl.ctx);
-  if (at >= at_end || !find_unit(p, at, tid_lane, &pl)) return;
+  if (at >= at_end || !find_unit(p, lens, at, tid_lane, &pl)) return;
   }
 }
 
 // ---- combine ------------------------------------------------------------------------
-// A workgroup per (row, KV head, sequence): the parts' normalized outputs weighted by their
-// softmax sums.  Four waves take every fourth part.
+// The row's parts weighted by their softmax sums: lane i holds part i's reference and sum (64 parts
+// at a time), merged over the wave; every wave of a workgroup does this for itself.
+struct Merged {
+  float m, l;                       // largest reference, sum relative to it
+};
+__device__ __forceinline__ float wave_max(float v) {
+#pragma unroll
+  for (int o = 1; o < 16; o <<= 1) v = fmaxf(v, __shfl_xor(v, o));
+  return quad_max(v);
+}
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+  for (int o = 1; o < 16; o <<= 1) v += __shfl_xor(v, o);
+  return quad_sum(v);
+}
+__device__ __forceinline__ Merged merge_row(const DenseAttnParams& p, int first, int count, int g,
+                                            int row, int lane) {
+  float m = -__builtin_inff(), l = 0.0f;
+  for (int i = lane; i < count; i += 64) {
+    const Pair ml = p.part_ml[((int64_t)(first + i) * p.c.n_kv + g) * p.rows + row];
+    const float mn = fmaxf(m, ml.x);
+    l = (m == mn ? l : l * exp2_fast(m - mn)) + (ml.x == mn ? ml.y : ml.y * exp2_fast(ml.x - mn));
+    m = mn;
+  }
+  const float M = wave_max(m);
+  return {M, wave_sum(m == M ? l : l * exp2_fast(m - M))};
+}
+
+// w_j += sum over rows and over block j's subtiles of sum * 2^(reference - M_row) / L_row, for
+// 256 blocks of a KV head.
+__device__ __forceinline__ void gather_weights(const DenseAttnParams& p, int tile, int g, int b,
+                                               float* sM, float* sI) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int first, count, ctx;
+  slots_of(p, b, lane, &first, &count, &ctx);
+  const int64_t head = (int64_t)b * p.c.n_kv + g;
+  const int sub_shift = p.c.shift - 4, subs = (ctx + 15) >> 4;
+  if (tile * (256 << sub_shift) >= subs) return;
+  for (int row = wave; row < p.rows; row += 4) {
+    Merged t = {0.0f, 0.0f};
+    if (row_limit(p, b, ctx, row) > 0) t = merge_row(p, first, count, g, row, lane);
+    if (lane == 0) {
+      sM[row] = t.m;
+      sI[row] = t.l == 0.0f ? 0.0f : 1.0f / t.l;
+    }
+  }
+  __syncthreads();
+  const int j = tile * 256 + threadIdx.x, s0 = j << sub_shift;
+  if (s0 >= subs) return;
+  const int n = (min(s0 + (1 << sub_shift), subs) - s0) * p.rows;
+  const Pair* y = p.sub + (head * p.sub_per_head + s0) * p.rows;
+  float w = 0.0f;
+  int row = 0;
+#pragma unroll 8
+  for (int i = 0; i < n; ++i) {
+    const Pair v = y[i];
+    // (a row without tokens or without a query has weight 0 whatever its reference)
+    w += v.x == 0.0f || sI[row] == 0.0f ? 0.0f : v.x * exp2_fast(v.y - sM[row]) * sI[row];
+    row = row + 1 == p.rows ? 0 : row + 1;
+  }
+  p.weights[head * p.c.blocks_per_head + j] += w;
+}
+
+// A workgroup per (row, KV head, sequence); its four waves take every fourth part.  Workgroups
+// past the rows gather the weights.
 template <int D>
 __global__ __launch_bounds__(256) void dense_combine_kernel(const DenseAttnParams p) {
   constexpr int C = D / 64;
-  __shared__ float so[4][D], sm[4], sl[4];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  __shared__ float so[4][D], sM[64], sI[64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int row = blockIdx.x, g = blockIdx.y, b = blockIdx.z;
-  const int ctx = clamp_ctx(p, b);
-  const int lim = row_limit(p, b, ctx, row);
-  if (lim < 0) return;
-  int first, count;
-  slots_of(p, b, lane, &first, &count);
-  // this wave's parts: their largest reference and sum
-  float m = -__builtin_inff(), l = 0.0f, o[C] = {};
+  if (row >= p.rows) {
+    gather_weights(p, row - p.rows, g, b, sM, sI);
+    return;
+  }
+  int first, count, ctx;
+  slots_of(p, b, lane, &first, &count, &ctx);
+  if (row_limit(p, b, ctx, row) < 0) return;
+  const Merged t = merge_row(p, first, count, g, row, lane);
+  float o[C] = {};
+#pragma unroll 4
   for (int i = wave; i < count; i += 4) {
     const int64_t slot = ((int64_t)(first + i) * p.c.n_kv + g) * p.rows + row;
     const Pair ml = p.part_ml[slot];
-    const float mn = fmaxf(m, ml.x);
-    const float a = m == mn ? 1.0f : exp2_fast(m - mn);
-    const float f = ml.x == mn ? ml.y : ml.y * exp2_fast(ml.x - mn);
-    m = mn;
-    l = l * a + f;
+    const float f = ml.x == t.m ? ml.y : ml.y * exp2_fast(ml.x - t.m);
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       const float v = p.part_o[slot * D + c * 64 + lane];
-      o[c] = o[c] * a + (f == 0.0f ? 0.0f : f * v);
+      o[c] += f == 0.0f ? 0.0f : f * v;
     }
   }
-  if (lane == 0) { sm[wave] = m; sl[wave] = l; }
 #pragma unroll
   for (int c = 0; c < C; ++c) so[wave][c * 64 + lane] = o[c];
   __syncthreads();
-  const float M = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3]));
-  float f[4], L = 0.0f;
-#pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    f[w] = sm[w] == M ? 1.0f : exp2_fast(sm[w] - M);
-    L += sl[w] * f[w];
-  }
   if (threadIdx.x < D) {
-    float v = 0.0f;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) v += so[w][threadIdx.x] * f[w];
-    v = L == 0.0f ? 0.0f : v / L;
+    const int i = threadIdx.x;
+    float v = (so[0][i] + so[1][i]) + (so[2][i] + so[3][i]);
+    v = t.l == 0.0f ? 0.0f : v / t.l;
     const int jq = row / p.group, iq = row % p.group;
     uint16_t* out = p.out + b * p.os_b + jq * p.os_t + (g * p.group + iq) * p.os_h;
-    out[threadIdx.x] = p.c.bf16 ? __builtin_bit_cast(uint16_t, (__bf16)v)
-                                : __builtin_bit_cast(uint16_t, (_Float16)v);
+    out[i] = p.c.bf16 ? __builtin_bit_cast(uint16_t, (__bf16)v)
+                      : __builtin_bit_cast(uint16_t, (_Float16)v);
   }
-}
-
-// ---- weights ------------------------------------------------------------------------
-// w_j += sum over rows and over the block's subtiles of sum * 2^(reference - M_row) / L_row.
-// A workgroup per 256 blocks of a KV head; it merges the rows' references and sums first.
-__global__ __launch_bounds__(256) void dense_weights_kernel(const DenseAttnParams p) {
-  __shared__ float sM[64], sI[64];
-  const int lane = threadIdx.x & 63;
-  const int g = blockIdx.y, b = blockIdx.z;
-  const int ctx = clamp_ctx(p, b);
-  const int64_t head = (int64_t)b * p.c.n_kv + g;
-  const int j = blockIdx.x * 256 + threadIdx.x;
-  const int per = 1 << (p.c.shift - 4);
-  const int subs = (ctx + 15) >> 4;
-  if (blockIdx.x * 256 * per >= subs) return;
-  int first, count;
-  slots_of(p, b, lane, &first, &count);
-  for (int row = threadIdx.x; row < p.rows; row += 256) {
-    float M = -__builtin_inff(), L = 0.0f;
-    if (row_limit(p, b, ctx, row) > 0) {
-      for (int i = 0; i < count; ++i) {
-        const Pair ml = p.part_ml[((int64_t)(first + i) * p.c.n_kv + g) * p.rows + row];
-        const float mn = fmaxf(M, ml.x);
-        L = (M == mn ? L : L * exp2_fast(M - mn)) + (ml.x == mn ? ml.y : ml.y * exp2_fast(ml.x - mn));
-        M = mn;
-      }
-    }
-    sM[row] = M;
-    sI[row] = L == 0.0f ? 0.0f : 1.0f / L;
-  }
-  __syncthreads();
-  if (j * per >= subs) return;
-  float w = 0.0f;
-  for (int r = 0; r < p.rows; ++r) {
-    if (sI[r] == 0.0f) continue;
-    float x = 0.0f;
-    for (int k = 0; k < per && j * per + k < subs; ++k) {
-      const Pair y = p.sub[(head * p.sub_per_head + j * per + k) * p.rows + r];
-      x += y.x == 0.0f ? 0.0f : y.x * exp2_fast(y.y - sM[r]);
-    }
-    w += x * sI[r];
-  }
-  p.weights[head * p.c.blocks_per_head + j] += w;
 }
 
 template <int D, bool E4M3, int RT>
@@ -714,14 +766,10 @@ int launch_dense_attn(const DenseAttnParams& p, void* stream) {
   }
   int e = (int)hipGetLastError();
   if (e) return e;
-  const dim3 grid(p.rows, p.c.n_kv, p.c.batch);
+  const int J = (p.max_ctx + (1 << p.c.shift) - 1) >> p.c.shift;
+  const dim3 grid(p.rows + (p.weights ? (J + 255) / 256 : 0), p.c.n_kv, p.c.batch);
   if (p.c.d == 128) hipLaunchKernelGGL(dense_combine_kernel<128>, grid, dim3(256), 0, st, p);
   else hipLaunchKernelGGL(dense_combine_kernel<64>, grid, dim3(256), 0, st, p);
-  e = (int)hipGetLastError();
-  if (e || !p.weights) return e;
-  const int J = (p.max_ctx + (1 << p.c.shift) - 1) >> p.c.shift;
-  hipLaunchKernelGGL(dense_weights_kernel, dim3((J + 255) / 256, p.c.n_kv, p.c.batch), dim3(256), 0,
-                     st, p);
   return (int)hipGetLastError();
 }
 
