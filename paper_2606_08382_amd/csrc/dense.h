@@ -87,6 +87,10 @@ struct DenseAttnParams {
   float scale_log2;                             // softmax scale * log2(e)
 };
 
+// Query rows of a KV head that the split kernel takes; above them the chunk kernel, in row tiles.
+constexpr int kSplitRows = 64;
+constexpr int kChunkRows = 128;
+
 int launch_rope(const RopeParams& p, bool wide, void* stream);
 int launch_dense_append(const DenseAppendParams& p, void* stream);
 int launch_dense_read(const DenseReadParams& p, void* stream);

@@ -238,11 +238,263 @@ __device__ __forceinline__ void raise(State<D, RT>& s, const float* top, float s
   }
 }
 
-template <int D, bool E4M3, int RT, bool SUMS>
-__global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void dense_split_kernel(const DenseAttnParams p) {
-  constexpr int N = D / 64, CT = D / 16, NB = RT == 1 ? 3 : 2;
+// Where a split pass with weights leaves the sums of 16-token subtiles.
+struct SubSums {
+  Pair* at;                         // of the KV head's first subtile, row 0
+  int row0, rows;                   // the wave's first row; rows of the KV head
+};
+
+// Probabilities pr of a 32-token step of tokens t.. from its log2 scores x (tokens from lim[] on,
+// and from `end` on, are absent), added to the running sums; sv: value scales of its subtiles.
+// A lane's tokens are t + 16 a + 4 quad + e, a = 0, 1, e = 0..3, for column col of each row tile.
+template <int D, int RT, bool SUMS>
+__device__ __forceinline__ void softmax_step(State<D, RT>& s, f4 (&x)[RT][2], const int (&lim)[RT],
+                                             int lim_lo, int t, int end, float sv0, float sv1,
+                                             int col, int quad, const SubSums& sums,
+                                             float (&pr)[RT][8]) {
+  if (t + 32 > lim_lo || t + 32 > end) {
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+      for (int a = 0; a < 2; ++a)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int tok = t + a * 16 + quad * 4 + e;
+          x[r][a][e] = tok < lim[r] && tok < end ? x[r][a][e] : -__builtin_inff();
+        }
+  }
+  float top[RT];
+  bool over = fmaxf(sv0, sv1) > s.vref;
+#pragma unroll
+  for (int r = 0; r < RT; ++r) {
+    top[r] = fmaxf(fmaxf(fmaxf(x[r][0][0], x[r][0][1]), fmaxf(x[r][0][2], x[r][0][3])),
+                   fmaxf(fmaxf(x[r][1][0], x[r][1][1]), fmaxf(x[r][1][2], x[r][1][3])));
+    over |= top[r] > s.m[r] + kAbove;
+  }
+  if (__any(over)) raise(s, top, fmaxf(sv0, sv1));
+#pragma unroll
+  for (int r = 0; r < RT; ++r) {
+    // a column that has seen nothing keeps reference -inf: x - 0 is -inf, its exponential 0
+    const float m = s.m[r] == -__builtin_inff() ? 0.0f : s.m[r];
+#pragma unroll
+    for (int a = 0; a < 2; ++a) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) pr[r][a * 4 + e] = exp2_fast(x[r][a][e] - m);
+      const float part = (pr[r][a * 4] + pr[r][a * 4 + 1]) + (pr[r][a * 4 + 2] + pr[r][a * 4 + 3]);
+      s.l[r] += part;
+      if constexpr (SUMS) {
+        const float y = quad_sum(part);
+        const int row = sums.row0 + r * 16 + col;
+        if (quad == 0 && row < sums.rows && t + a * 16 < end)
+          sums.at[(int64_t)((t >> 4) + a) * sums.rows + row] = {y, s.m[r]};
+      }
+    }
+  }
+}
+
+// Probabilities of a step of finished blocks as the products' fp16 operand.
+template <int RT>
+__device__ __forceinline__ void scale_probs(const float (&pr)[RT][8], float f0, float f1, bool masked,
+                                            h8 (&ph)[RT]) {
+#pragma unroll
+  for (int r = 0; r < RT; ++r)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) ph[r][e] = (_Float16)(pr[r][e] * (e < 4 ? f0 : f1));
+  if (masked) {
+    // an absent token's probability is zero whatever its block's scale
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) ph[r][e] = pr[r][e] == 0.0f ? (_Float16)0.0f : ph[r][e];
+  }
+}
+
+// Query rows row0 + 16 r + col, channels i*64 + quad*16 + h*8 + e (operand n = 2 i + h), as given.
+union Raw {
+  u4 v;
+  uint16_t h[8];
+};
+__device__ __forceinline__ u4 load_query(const DenseAttnParams& p, int b, int g, int row, int ch) {
+  const int jq = row / p.group, iq = row % p.group;
+  const uint16_t* src = p.q + b * p.qs_b + jq * p.qs_t + (g * p.group + iq) * p.qs_h + ch;
+  Raw w;
+  if (p.q_wide) {
+    w.v = *reinterpret_cast<const u4*>(src);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w.h[e] = src[e];
+  }
+  return w.v;
+}
+template <int D, int RT>
+__device__ __forceinline__ void load_queries(const DenseAttnParams& p, int b, int g, int row0, int col,
+                                             int quad, const int (&lm)[RT], Raw (&raw)[RT][D / 32]) {
+#pragma unroll
+  for (int r = 0; r < RT; ++r)
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+      raw[r][i].v = lm[r] < 0 ? (u4){0, 0, 0, 0}
+                              : load_query(p, b, g, row0 + r * 16 + col,
+                                           (i >> 1) * 64 + quad * 16 + (i & 1) * 8);
+}
+// The same as fp16, scaled by a power of two per row; qs: what then makes a score a log2 score.
+template <int D, int RT>
+__device__ __forceinline__ void scale_queries(const DenseAttnParams& p, const Raw (&raw)[RT][D / 32],
+                                              h8 (&q)[RT][D / 32], float (&qs)[RT]) {
+#pragma unroll
+  for (int r = 0; r < RT; ++r) {
+    float top = 0.0f;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(from16(raw[r][i].h[e], p.c.bf16)));
+    top = quad_max(top);
+    const int ex = top > 0.0f && top < __builtin_inff() ? 8 - __builtin_amdgcn_frexp_expf(top) : 0;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        q[r][i][e] = (_Float16)__builtin_amdgcn_ldexpf(from16(raw[r][i].h[e], p.c.bf16), ex);
+    qs[r] = __builtin_amdgcn_ldexpf(p.scale_log2, -ex);
+  }
+}
+
+__device__ __forceinline__ f4 mfma_raw(u4 a, u4 b, f4 c, int bf16) {
+  return bf16 ? mfma_bf16(__builtin_bit_cast(b8, a), __builtin_bit_cast(b8, b), c)
+              : mfma_f16(__builtin_bit_cast(h8, a), __builtin_bit_cast(h8, b), c);
+}
+
+// The unfinished block, from its 16-bit rows: 32-token steps at t0, t0 + stride, .. below `end`
+// (of ctx tokens).  Operands are the stored type; a bf16 probability is split in two parts.
+// A value that is not finite is left out of the product, where it would reach rows that do not
+// see its token; the rows that do get NaN in its channel.
+template <int D, int RT, bool SUMS>
+__device__ __forceinline__ void unfinished_block(const DenseAttnParams& p, State<D, RT>& s, int b, int g,
+                                                 int ctx, int end, int t0, int stride, int row0,
+                                                 const int (&lim)[RT], int lim_lo,
+                                                 const SubSums& sums, int lane) {
+  constexpr int CT = D / 16;
+  const int col = lane & 15, quad = lane >> 4, T = 1 << p.c.shift, bf16 = p.c.bf16;
+  const uint16_t* kt = p.c.tails + ((int64_t)b * p.c.n_kv + g) * 2 * (2 * T * D);
+  const uint16_t* vt = kt + 2 * T * D;
+  for (int t = t0; t < end; t += stride) {
+    f4 sc[RT][2];
+#pragma unroll
+    for (int r = 0; r < RT; ++r) sc[r][0] = sc[r][1] = (f4){0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) {
+      const int ch = (i >> 1) * 64 + quad * 16 + (i & 1) * 8;
+      u4 k[2];
+#pragma unroll
+      for (int a = 0; a < 2; ++a) {
+        const int tok = t + a * 16 + col;
+        k[a] = tok < ctx ? *reinterpret_cast<const u4*>(kt + (tok & (2 * T - 1)) * D + ch)
+                         : (u4){0, 0, 0, 0};
+      }
+#pragma unroll
+      for (int r = 0; r < RT; ++r) {
+        u4 q = {0, 0, 0, 0};
+        if (lim[r] != 0x7fffffff) q = load_query(p, b, g, row0 + r * 16 + col, ch);
+#pragma unroll
+        for (int a = 0; a < 2; ++a) sc[r][a] = mfma_raw(k[a], q, sc[r][a], bf16);
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+      sc[r][0] *= p.scale_log2;
+      sc[r][1] *= p.scale_log2;
+    }
+    float pr[RT][8];
+    softmax_step<D, RT, SUMS>(s, sc, lim, lim_lo, t, ctx, 1.0f, 1.0f, col, quad, sums, pr);
+    u4 pa[RT], pb[RT];                              // fp16; or two bf16 parts
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+      union { _Float16 h[8]; __bf16 b[8]; u4 v; } hi, lo;
+      lo.v = (u4){0, 0, 0, 0};
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float x = pr[r][e] * s.vinv;
+        if (bf16) {
+          hi.b[e] = (__bf16)x;
+          lo.b[e] = (__bf16)(x - (float)hi.b[e]);
+        } else {
+          hi.h[e] = (_Float16)x;
+        }
+      }
+      pa[r] = hi.v;
+      pb[r] = lo.v;
+    }
+    const uint32_t inf16 = bf16 ? 0x7f80u : 0x7c00u, one = bf16 ? 0x3f80u : 0x3c00u;
+#pragma unroll
+    for (int c0 = 0; c0 < CT; c0 += 4) {
+      // values: tokens t + 16 a + 4 quad .. + 3 of channel 16 c + col; absent ones cleared
+      u4 v[4];
+      uint32_t top = 0;
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int a = 0; a < 2; ++a) {
+          const int tok = t + a * 16 + quad * 4, rr = tok & (2 * T - 1);
+          u2 w = {0, 0};
+          if (tok < ctx) {
+            w = *reinterpret_cast<const u2*>(vt + ((rr >> 4) * D + (c0 + c) * 16 + col) * 16 + quad * 4);
+            const int left = ctx - tok;
+            if (left < 2) w.x &= 0xffffu;
+            if (left < 3) w.y = 0;
+            else if (left < 4) w.y &= 0xffffu;
+          }
+          v[c][2 * a] = w.x;
+          v[c][2 * a + 1] = w.y;
+        }
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          top = max(top, max((v[c][i] & 0x7fffu) << 16, v[c][i] & 0x7fff0000u));
+      if (__any(top >= inf16 << 16)) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          u4 bad;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const bool lo = (v[c][i] & 0x7fffu) >= inf16, hi = (v[c][i] >> 16 & 0x7fffu) >= inf16;
+            bad[i] = (lo ? one : 0) | (hi ? one << 16 : 0);
+            v[c][i] &= (lo ? 0 : 0xffffu) | (hi ? 0 : 0xffff0000u);
+          }
+#pragma unroll
+          for (int r = 0; r < RT; ++r) {
+            u4 sees;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int tok = t + (i >> 1) * 16 + quad * 4 + (i & 1) * 2;
+              sees[i] = (tok < lim[r] ? one : 0) | (tok + 1 < lim[r] ? one << 16 : 0);
+            }
+            const f4 n = mfma_raw(bad, sees, (f4){0.0f, 0.0f, 0.0f, 0.0f}, bf16);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              s.o[r][c0 + c][e] = n[e] > 0.0f ? __builtin_nanf("") : s.o[r][c0 + c][e];
+          }
+        }
+      }
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+          s.o[r][c0 + c] = mfma_raw(v[c], pa[r], s.o[r][c0 + c], bf16);
+          if (bf16) s.o[r][c0 + c] = mfma_raw(v[c], pb[r], s.o[r][c0 + c], 1);
+        }
+    }
+  }
+}
+
+// Up to 64 query rows of a KV head.  A workgroup's waves take 32-token steps in turn; with RG = 2
+// two row groups of 16 RT rows share the steps (a wave's state of 64 rows would leave one wave
+// per SIMD; the codes' second reader finds them in cache).
+template <int D, bool E4M3, int RT, int RG, bool SUMS>
+__global__ __launch_bounds__(256, 2) void dense_split_kernel(const DenseAttnParams p) {
+  constexpr int N = D / 64, CT = D / 16, NB = RT == 1 ? 3 : 2, TW = kWavesA / RG, kRound = 32 * TW;
   const int tid_lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int g = blockIdx.y, row0 = blockIdx.z * (16 * RT);
+  const int token_wave = wave / RG, row0 = wave % RG * (16 * RT), g = blockIdx.y;
   const Lens lens = first_lens(p, tid_lane);
   const int R = range_units(p, lens, tid_lane);
   __shared__ float so[kWavesA][16][D + 4];
@@ -264,13 +516,13 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void dense_split_kernel(const
   it.t1 = min(min(at_end - pl.start, units_of(pl.ctx)) * kUnit, pl.ctx);
   const int full = it.ctx & ~(T - 1);
   const int64_t head = (int64_t)it.b * p.c.n_kv + g;
-  const int e8 = min(it.t1, full), tw = it.t0 + 32 * wave;   // the wave's finished blocks
+  const int e8 = min(it.t1, full), tw = it.t0 + 32 * token_wave;   // the wave's finished blocks
 
   // The chains of loads that a part begins with overlap: the table entries of the first 64 steps
   // (a subtile per lane and 32 steps), the queries, then the entries' scales and codes.
   const int32_t* table = p.c.table + head * p.c.blocks_per_head;
   auto entry_token = [&](int i0) {
-    return max(min(tw + (i0 + (lane >> 1)) * kUnit + (lane & 1) * 16, e8 - 16), 0);
+    return max(min(tw + (i0 + (lane >> 1)) * kRound + (lane & 1) * 16, e8 - 16), 0);
   };
   const int entry0 = table[entry_token(0) >> sh], entry1 = table[entry_token(32) >> sh];
 
@@ -278,44 +530,21 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void dense_split_kernel(const
   h8 q[RT][2 * N];
   float qs[RT];
   int lim[RT];
-  int lim_lo = 0x7fffffff, lim_hi = 0;
-  union Raw { u4 v; uint16_t h[8]; };
-  Raw raw[RT][2 * N];
+  int lm[RT];
+  int lim_lo = 0x7fffffff;
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
-    const int row = row0 + r * 16 + col;
-    const int lm = row_limit(p, it.b, it.ctx, row);
-    lim[r] = lm < 0 ? 0x7fffffff : lm;             // rows without a query see everything
+    lm[r] = row_limit(p, it.b, it.ctx, row0 + r * 16 + col);
+    lim[r] = lm[r] < 0 ? 0x7fffffff : lm[r];       // rows without a query see everything
     lim_lo = min(lim_lo, lim[r]);
-    lim_hi = max(lim_hi, lm);
-    const int jq = row / p.group, iq = row % p.group;
-    const uint16_t* src = p.q + it.b * p.qs_b + jq * p.qs_t + (g * p.group + iq) * p.qs_h;
-#pragma unroll
-    for (int i = 0; i < 2 * N; ++i) {
-      const int ch = (i >> 1) * 64 + quad * 16 + (i & 1) * 8;
-      raw[r][i].v = (u4){0, 0, 0, 0};
-      if (lm >= 0) {
-        if (p.q_wide) {
-          raw[r][i].v = *reinterpret_cast<const u4*>(src + ch);
-        } else {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) raw[r][i].h[e] = src[ch + e];
-        }
-      }
-    }
   }
+  Raw raw[RT][2 * N];
+  load_queries<D, RT>(p, it.b, g, row0, col, quad, lm, raw);
 #pragma unroll
-  for (int o = 8; o >= 1; o >>= 1) {
-    lim_lo = min(lim_lo, __shfl_xor(lim_lo, o));
-    lim_hi = max(lim_hi, __shfl_xor(lim_hi, o));
-  }
+  for (int o = 8; o >= 1; o >>= 1) lim_lo = min(lim_lo, __shfl_xor(lim_lo, o));
   lim_lo = __builtin_amdgcn_readfirstlane(lim_lo);
-  lim_hi = __builtin_amdgcn_readfirstlane(lim_hi);
 
-  // row tiles of early query tokens end before the sequence does; a part's sums are written for
-  // all of its subtiles
-  const int stop = SUMS ? e8 : min(e8, (lim_hi + 15) & ~15);
-  const int steps = stop > tw ? (stop - tw + kUnit - 1) / kUnit : 0;
+  const int steps = e8 > tw ? (e8 - tw + kRound - 1) / kRound : 0;
   struct Entry { uint32_t sub; float sk, sv; };
   auto entry_of = [&](int e, int i0) {
     const int t = entry_token(i0);
@@ -360,23 +589,7 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void dense_split_kernel(const
     for (int u = 0; u < NB - 1; ++u) fetch(x[u], u);
   }
 
-  // queries as fp16, scaled by a power of two per row
-#pragma unroll
-  for (int r = 0; r < RT; ++r) {
-    float top = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 2 * N; ++i)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(from16(raw[r][i].h[e], p.c.bf16)));
-    top = quad_max(top);
-    const int ex = top > 0.0f && top < __builtin_inff() ? 8 - __builtin_amdgcn_frexp_expf(top) : 0;
-#pragma unroll
-    for (int i = 0; i < 2 * N; ++i)
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        q[r][i][e] = (_Float16)__builtin_amdgcn_ldexpf(from16(raw[r][i].h[e], p.c.bf16), ex);
-    qs[r] = __builtin_amdgcn_ldexpf(p.scale_log2, -ex);
-  }
+  scale_queries<D, RT>(p, raw, q, qs);
 
   State<D, RT> s;
 #pragma unroll
@@ -389,54 +602,10 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void dense_split_kernel(const
   s.vref = kTinyScale;
   s.vinv = 1.0f / kTinyScale;
 
-  // Softmax of a step's scores and its product with the values.  x: log2 scores; t: first token;
-  // sv: value scales of the two subtiles; pv(r, pr): the product.  Scores of tokens from lim
-  // on, and from `end` on, count as absent.
-  auto softmax = [&](f4 (&x)[RT][2], int t, int end, const float* sv, float (&pr)[RT][8], bool odd) {
-    if (t + 32 > lim_lo || t + 32 > end) {
-#pragma unroll
-      for (int r = 0; r < RT; ++r)
-#pragma unroll
-        for (int a = 0; a < 2; ++a)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int tok = t + a * 16 + quad * 4 + e;
-            x[r][a][e] = tok < lim[r] && tok < end ? x[r][a][e] : -__builtin_inff();
-          }
-    }
-    float top[RT];
-    bool over = fmaxf(sv[0], sv[1]) > s.vref;
-#pragma unroll
-    for (int r = 0; r < RT; ++r) {
-      top[r] = fmaxf(fmaxf(fmaxf(x[r][0][0], x[r][0][1]), fmaxf(x[r][0][2], x[r][0][3])),
-                     fmaxf(fmaxf(x[r][1][0], x[r][1][1]), fmaxf(x[r][1][2], x[r][1][3])));
-      over |= top[r] > s.m[r] + kAbove;
-    }
-    if (__any(over)) raise(s, top, fmaxf(sv[0], sv[1]));
-#pragma unroll
-    for (int r = 0; r < RT; ++r) {
-      // a column that has seen nothing keeps reference -inf: x - 0 is -inf, its exponential 0
-      const float m = s.m[r] == -__builtin_inff() ? 0.0f : s.m[r];
-      float part[2];
-#pragma unroll
-      for (int a = 0; a < 2; ++a) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) pr[r][a * 4 + e] = exp2_fast(x[r][a][e] - m);
-        part[a] = (pr[r][a * 4] + pr[r][a * 4 + 1]) + (pr[r][a * 4 + 2] + pr[r][a * 4 + 3]);
-        s.l[r] += part[a];
-        if constexpr (SUMS) {
-          const float y = quad_sum(part[a]);
-          const int row = r * 16 + col;
-          if (quad == 0 && row < p.rows && (a == 0 || odd))
-            p.sub[(head * p.sub_per_head + (t >> 4) + a) * p.rows + row] = {y, s.m[r]};
-        }
-      }
-    }
-  };
-
+  const SubSums sums = {SUMS ? p.sub + head * p.sub_per_head * p.rows : nullptr, row0, p.rows};
   // ---- finished blocks
   auto compute = [&](const Tile<D>& y, int i) {
-    const int t = tw + i * kUnit;
+    const int t = tw + i * kRound;
     f4 sc[RT][2];
 #pragma unroll
     for (int a = 0; a < 2; ++a) {
@@ -454,20 +623,9 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void dense_split_kernel(const
       for (int r = 0; r < RT; ++r) sc[r][a] *= y.sk[a] * qs[r];
     }
     float pr[RT][8];
-    softmax(sc, t, e8, y.sv, pr, t + 16 < e8);
+    softmax_step<D, RT, SUMS>(s, sc, lim, lim_lo, t, e8, y.sv[0], y.sv[1], col, quad, sums, pr);
     h8 ph[RT];
-    const float f0 = y.sv[0] * s.vinv, f1 = y.sv[1] * s.vinv;
-#pragma unroll
-    for (int r = 0; r < RT; ++r)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) ph[r][e] = (_Float16)(pr[r][e] * (e < 4 ? f0 : f1));
-    if (t + 32 > lim_lo || t + 32 > e8) {
-      // an absent token's probability is zero whatever its block's scale
-#pragma unroll
-      for (int r = 0; r < RT; ++r)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) ph[r][e] = pr[r][e] == 0.0f ? (_Float16)0.0f : ph[r][e];
-    }
+    scale_probs<RT>(pr, y.sv[0] * s.vinv, y.sv[1] * s.vinv, t + 32 > lim_lo || t + 32 > e8, ph);
 #pragma unroll
     for (int n = 0; n < N; ++n)
 #pragma unroll
@@ -487,102 +645,14 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void dense_split_kernel(const
     }
   }
 
-  // ---- the unfinished block, from its 16-bit rows
-  if (full < it.t1 && (SUMS || lim_hi > full)) {
-    lane = fresh(tid_lane);
-    col = lane & 15;
-    quad = lane >> 4;
-    const uint16_t* kt = p.c.tails + head * 2 * (2 * T * D);
-    const uint16_t* vt = kt + 2 * T * D;
-    for (int t = full + 32 * wave; t < it.ctx; t += kUnit) {
-      f4 sc[RT][2];
-      const int bf16 = p.c.bf16;
-#pragma unroll
-      for (int r = 0; r < RT; ++r) sc[r][0] = sc[r][1] = (f4){0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-      for (int n = 0; n < 2 * N; ++n) {
-        const int ch = n * 32 + quad * 8;
-        u4 k[2];
-#pragma unroll
-        for (int a = 0; a < 2; ++a) {
-          const int tok = t + a * 16 + col;
-          k[a] = tok < it.ctx ? *reinterpret_cast<const u4*>(kt + (tok & (2 * T - 1)) * D + ch)
-                              : (u4){0, 0, 0, 0};
-        }
-#pragma unroll
-        for (int r = 0; r < RT; ++r) {
-          // the query row as it was given
-          const int row = row0 + r * 16 + col, jq = row / p.group, iq = row % p.group;
-          const uint16_t* src = p.q + it.b * p.qs_b + jq * p.qs_t + (g * p.group + iq) * p.qs_h + ch;
-          union { u4 v; uint16_t h[8]; } w;
-          w.v = (u4){0, 0, 0, 0};
-          if (lim[r] != 0x7fffffff) {
-            if (p.q_wide) {
-              w.v = *reinterpret_cast<const u4*>(src);
-            } else {
-#pragma unroll
-              for (int e = 0; e < 8; ++e) w.h[e] = src[e];
-            }
-          }
-#pragma unroll
-          for (int a = 0; a < 2; ++a)
-            sc[r][a] = bf16 ? mfma_bf16(__builtin_bit_cast(b8, k[a]), __builtin_bit_cast(b8, w.v), sc[r][a])
-                            : mfma_f16(__builtin_bit_cast(h8, k[a]), __builtin_bit_cast(h8, w.v), sc[r][a]);
-        }
-      }
-#pragma unroll
-      for (int r = 0; r < RT; ++r) {
-        sc[r][0] *= p.scale_log2;
-        sc[r][1] *= p.scale_log2;
-      }
-      const float one[2] = {1.0f, 1.0f};
-      float pr[RT][8];
-      softmax(sc, t, it.ctx, one, pr, t + 16 < it.ctx);
-      h8 ph[RT];
-      b8 pb[RT][2];
-#pragma unroll
-      for (int r = 0; r < RT; ++r)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float v = pr[r][e] * s.vinv;
-          ph[r][e] = (_Float16)v;
-          pb[r][0][e] = (__bf16)v;
-          pb[r][1][e] = (__bf16)(v - (float)pb[r][0][e]);
-        }
-#pragma unroll
-      for (int c = 0; c < CT; ++c) {
-        u2 w[2];
-#pragma unroll
-        for (int a = 0; a < 2; ++a) {
-          // tokens t + 16a + 4 quad .. + 3 of channel 16c + col; absent ones cleared
-          const int tok = t + a * 16 + quad * 4, rr = tok & (2 * T - 1);
-          w[a] = (u2){0, 0};
-          if (tok < it.ctx) {
-            w[a] = *reinterpret_cast<const u2*>(vt + ((rr >> 4) * D + c * 16 + col) * 16 + quad * 4);
-            const int left = it.ctx - tok;
-            if (left < 2) w[a].x &= 0xffffu;
-            if (left < 3) w[a].y = 0;
-            else if (left < 4) w[a].y &= 0xffffu;
-          }
-        }
-        const u4 v = {w[0].x, w[0].y, w[1].x, w[1].y};
-#pragma unroll
-        for (int r = 0; r < RT; ++r) {
-          if (bf16) {
-            s.o[r][c] = mfma_bf16(__builtin_bit_cast(b8, v), pb[r][0], s.o[r][c]);
-            s.o[r][c] = mfma_bf16(__builtin_bit_cast(b8, v), pb[r][1], s.o[r][c]);
-          } else {
-            s.o[r][c] = mfma_f16(__builtin_bit_cast(h8, v), ph[r], s.o[r][c]);
-          }
-        }
-      }
-    }
-  }
+  if (full < it.t1)
+    unfinished_block<D, RT, SUMS>(p, s, it.b, g, it.ctx, it.ctx, full + 32 * token_wave, kRound, row0,
+                                  lim, lim_lo, sums, fresh(tid_lane));
 
   lane = fresh(tid_lane);
   col = lane & 15;
   quad = lane >> 4;
-  // ---- the waves' states merged, normalized and written as the part's partial
+  // ---- the token waves' states merged, normalized and written as the part's partial
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
     const float l = quad_sum(s.l[r]);
@@ -592,44 +662,261 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void dense_split_kernel(const
     }
   }
   __syncthreads();
-  const int64_t slot0 = ((int64_t)(blockIdx.x + it.b) * p.c.n_kv + g) * p.rows + row0;
+  const int64_t slot0 = ((int64_t)(blockIdx.x + it.b) * p.c.n_kv + g) * p.rows;
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
+    const int group = wave % RG;
     float M = -__builtin_inff();
 #pragma unroll
-    for (int w = 0; w < kWavesA; ++w) M = fmaxf(M, sm[w][r * 16 + col]);
+    for (int w = 0; w < TW; ++w) M = fmaxf(M, sm[w * RG + group][r * 16 + col]);
     float L = 0.0f, own = 0.0f;
 #pragma unroll
-    for (int w = 0; w < kWavesA; ++w) {
-      const float mw = sm[w][r * 16 + col], lw = sl[w][r * 16 + col];
+    for (int w = 0; w < TW; ++w) {
+      const float mw = sm[w * RG + group][r * 16 + col], lw = sl[w * RG + group][r * 16 + col];
       const float a = mw == M ? 1.0f : exp2_fast(mw - M);
       // a wave without tokens: sum 0 (NaN stays)
       L += lw * a;
-      if (w == wave) own = a;
+      if (w == token_wave) own = a;
     }
     const float f = L == 0.0f ? 0.0f : own / L;
-    if (wave == 0 && quad == 0 && row0 + r * 16 + col < p.rows)
-      p.part_ml[slot0 + r * 16 + col] = {M, L};
+    if (token_wave == 0 && quad == 0 && row0 + r * 16 + col < p.rows)
+      p.part_ml[slot0 + row0 + r * 16 + col] = {M, L};
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
-      f4 v = s.o[r][c] * f;                         // at most fp16's largest code, then the scale
+      f4 v = s.o[r][c] * f;                         // at most the largest code, then the scale
       v *= s.vref;
       *reinterpret_cast<f4*>(&so[wave][col][c * 16 + quad * 4]) = v;
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < 16 * D / 4; i += 256) {
-      const int row = i / (D / 4), ch = i % (D / 4) * 4;
-      if (row0 + r * 16 + row < p.rows) {
-        f4 v = *reinterpret_cast<const f4*>(&so[0][row][ch]);
+    for (int i = threadIdx.x; i < RG * 16 * D / 4; i += 256) {
+      const int gr = i / (16 * D / 4), row = i / (D / 4) % 16, ch = i % (D / 4) * 4;
+      const int to = gr * (16 * RT) + r * 16 + row;
+      if (to < p.rows) {
+        f4 v = *reinterpret_cast<const f4*>(&so[gr][row][ch]);
 #pragma unroll
-        for (int w = 1; w < kWavesA; ++w) v += *reinterpret_cast<const f4*>(&so[w][row][ch]);
-        *reinterpret_cast<f4*>(p.part_o + (slot0 + r * 16 + row) * D + ch) = v;
+        for (int w = 1; w < TW; ++w) v += *reinterpret_cast<const f4*>(&so[w * RG + gr][row][ch]);
+        *reinterpret_cast<f4*>(p.part_o + (slot0 + to) * D + ch) = v;
       }
     }
     __syncthreads();
   }
   at = pl.start + units_of(pl.ctx);
   if (at >= at_end || !find_unit(p, lens, at, tid_lane, &pl)) return;
+  }
+}
+
+// ---- chunk --------------------------------------------------------------------------
+// More than 64 query rows of a KV head: the matrix products bound it (4 d flops per row and token
+// against 2 d bytes per token).  A workgroup takes 128 rows, 32 a wave, so that a wave's state
+// and operands fit 256 registers and two workgroups share a compute unit: one's softmax runs
+// beside the other's products.  Tiles of 64 tokens are converted to fp16 once per workgroup, into
+// LDS in the operands' order (a wave's operand is 1 KiB in a row: no bank conflicts): two buffers,
+// one barrier a tile, the codes of the next tile already in registers.
+//
+// Workgroups of the same codes (row tiles of one KV head and range) have consecutive places on one
+// XCD, whose L2 then serves all but the first of them.
+constexpr int kTile = 64;                   // tokens
+
+template <int D, bool E4M3>
+__global__ __launch_bounds__(256, 2) void dense_chunk_kernel(const DenseAttnParams p) {
+  constexpr int N = D / 64, CT = D / 16, RT = 2;
+  constexpr int kFrag = 1024;               // bytes of a wave's operand
+  constexpr int kKeys = 4 * 2 * N * kFrag, kValues = 2 * CT * kFrag;
+  __shared__ __attribute__((aligned(16))) uint8_t lds[2][kKeys + kValues];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane & 15, quad = lane >> 4;
+  const int tiles = (p.rows + kChunkRows - 1) / kChunkRows;
+  // (range, KV head) pairs go round the XCDs, row tiles of a pair stay on one, the last (which
+  // sees most) first
+  const int xcd = blockIdx.x & 7, place = blockIdx.x >> 3;
+  const int pair = place / tiles * 8 + xcd, tile = tiles - 1 - place % tiles;
+  if (pair >= p.ranges * p.c.n_kv) return;
+  const int g = pair % p.c.n_kv, range = pair / p.c.n_kv;
+  const int row0 = tile * kChunkRows + wave * (16 * RT);
+  const int sh = p.c.shift, T = 1 << sh;
+  const Lens lens = first_lens(p, lane);
+  const int R = range_units(p, lens, lane);
+  Place pl;
+  int at = range * R;
+  const int at_end = at + R;
+  if (!find_unit(p, lens, at, lane, &pl)) return;
+  for (;;) {
+    const int b = pl.b, ctx = pl.ctx;
+    const int t0 = (at - pl.start) * kUnit;
+    const int t1 = min(min(at_end - pl.start, units_of(ctx)) * kUnit, ctx);
+    const int full = ctx & ~(T - 1);
+    const int64_t head = (int64_t)b * p.c.n_kv + g;
+    const int q_len = p.q_len ? min(max(p.q_len[b], 0), p.n_q) : p.n_q;
+    // query tokens of the workgroup's rows, and how far the last of them sees
+    const int j_lo = tile * kChunkRows / p.group;
+    const int j_hi = min((tile * kChunkRows + kChunkRows - 1) / p.group, q_len - 1);
+    const int sees = min(ctx - q_len + j_hi + 1, ctx);
+    if (j_lo < q_len) {
+      int lim[RT], lm[RT], lim_lo = 0x7fffffff;
+#pragma unroll
+      for (int r = 0; r < RT; ++r) {
+        lm[r] = row_limit(p, b, ctx, row0 + r * 16 + col);
+        lim[r] = lm[r] < 0 ? 0x7fffffff : lm[r];
+        lim_lo = min(lim_lo, lim[r]);
+      }
+#pragma unroll
+      for (int o = 8; o >= 1; o >>= 1) lim_lo = min(lim_lo, __shfl_xor(lim_lo, o));
+      lim_lo = __builtin_amdgcn_readfirstlane(lim_lo);
+      h8 q[RT][2 * N];
+      float qs[RT];
+      {
+        Raw raw[RT][2 * N];
+        load_queries<D, RT>(p, b, g, row0, col, quad, lm, raw);
+        scale_queries<D, RT>(p, raw, q, qs);
+      }
+      State<D, RT> s;
+#pragma unroll
+      for (int r = 0; r < RT; ++r) {
+        s.m[r] = -__builtin_inff();
+        s.l[r] = 0.0f;
+#pragma unroll
+        for (int c = 0; c < CT; ++c) s.o[r][c] = (f4){0.0f, 0.0f, 0.0f, 0.0f};
+      }
+      s.vref = kTinyScale;
+      s.vinv = 1.0f / kTinyScale;
+      const SubSums none = {nullptr, 0, 0};
+
+      const int e8 = min(min(t1, full), (sees + 15) & ~15);
+      const int n = e8 > t0 ? (e8 - t0 + kTile - 1) / kTile : 0;
+      const int32_t* table = p.c.table + head * p.c.blocks_per_head;
+      // entries of 16 tiles, a subtile per lane
+      struct Entry { uint32_t sub; float sk, sv; };
+      auto entries = [&](int i0) {
+        const int t = max(min(t0 + i0 * kTile + lane * 16, e8 - 16), 0);
+        const int e = min(max(table[t >> sh], 0), p.c.n_blocks - 1);
+        const Pair sc = p.c.scales[e];
+        return Entry{((uint32_t)e << (sh - 3)) + ((uint32_t)(t & (T - 1)) >> 4), sc.x, sc.y};
+      };
+      const uint32_t v_sub = (uint32_t)T >> 4;
+      // A thread's codes of a tile: key units tid + 256 i (subtile, then 16-byte unit); value units of
+      // the two subtiles of a 32-token step.
+      constexpr int kUnits = 16 * D / 16;           // 16-byte units of a subtile
+      constexpr int KL = 4 * kUnits / 256;          // 2 (D 128) or 1
+      u4 kc[KL], vc[2];
+      Entry now, next;
+      auto subtile = [&](const Entry& en, int i, int st) {
+        return (uint32_t)__builtin_amdgcn_readlane(en.sub, (i & 15) * 4 + st);
+      };
+      const int tid = threadIdx.x;
+      auto load = [&](const Entry& en, int i) {
+#pragma unroll
+        for (int k = 0; k < KL; ++k) {
+          const int u = wave * 64 + k * 256, st = u / kUnits;
+          kc[k] = *reinterpret_cast<const u4*>(p.c.codes + (uint64_t)subtile(en, i, st) * (16 * D) +
+                                               (u % kUnits + lane) * 16);
+        }
+        if (wave * 64 < 2 * kUnits) {
+          const int u = wave * 64, sp = u / kUnits;
+#pragma unroll
+          for (int a = 0; a < 2; ++a)
+            vc[a] = *reinterpret_cast<const u4*>(
+                p.c.codes + (uint64_t)(subtile(en, i, sp * 2 + a) + v_sub) * (16 * D) +
+                (u % kUnits + lane) * 16);
+        }
+      };
+      auto store = [&](uint8_t* buf) {
+#pragma unroll
+        for (int k = 0; k < KL; ++k) {
+          const int u = tid + k * 256, st = u / kUnits, w = u % kUnits, i = w >> 6;
+          uint8_t* to = buf + (st * 2 * N + 2 * i) * kFrag + (w & 63) * 16;
+          *reinterpret_cast<h8*>(to) = code8<E4M3>(kc[k][0], kc[k][1]);
+          *reinterpret_cast<h8*>(to + kFrag) = code8<E4M3>(kc[k][2], kc[k][3]);
+        }
+        if (wave * 64 < 2 * kUnits) {
+          const int sp = tid / kUnits, w = tid % kUnits, i = w >> 6;
+          uint8_t* to = buf + kKeys + (sp * CT + 4 * i) * kFrag + (w & 63) * 16;
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            *reinterpret_cast<h8*>(to + j * kFrag) = code8<E4M3>(vc[0][j], vc[1][j]);
+        }
+      };
+      __syncthreads();                              // the buffers' last readers are done
+      if (n > 0) {
+        now = entries(0);
+        next = entries(16);
+        load(now, 0);
+        store(lds[0]);
+        load(now, min(1, n - 1));
+      }
+      __syncthreads();
+      for (int i = 0; i < n; ++i) {
+        // the scales of this tile (its entries may be replaced below)
+        float sk[4], sv[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int l = (i & 15) * 4 + k;
+          sk[k] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(now.sk), l));
+          sv[k] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(now.sv), l));
+        }
+        if (i + 1 < n) store(lds[(i + 1) & 1]);
+        if (((i + 1) & 15) == 0) {
+          now = next;
+          next = entries(i + 17);
+        }
+        // (tile i + 2 lies in the next 16 when i + 1 ends these)
+        if (i + 2 < n) load(((i + 2) & 15) == 0 ? next : now, i + 2);
+        const uint8_t* buf = lds[i & 1];
+        const int t = t0 + i * kTile;
+#pragma unroll
+        for (int st = 0; st < 2; ++st) {
+          f4 sc[RT][2];
+#pragma unroll
+          for (int a = 0; a < 2; ++a) {
+#pragma unroll
+            for (int r = 0; r < RT; ++r) sc[r][a] = (f4){0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int k = 0; k < 2 * N; ++k) {
+              const h8 kf = *reinterpret_cast<const h8*>(buf + ((st * 2 + a) * 2 * N + k) * kFrag + lane * 16);
+#pragma unroll
+              for (int r = 0; r < RT; ++r) sc[r][a] = mfma_f16(kf, q[r][k], sc[r][a]);
+            }
+#pragma unroll
+            for (int r = 0; r < RT; ++r) sc[r][a] *= sk[st * 2 + a] * qs[r];
+          }
+          float pr[RT][8];
+          const int ts = t + st * 32;
+          softmax_step<D, RT, false>(s, sc, lim, lim_lo, ts, e8, sv[st * 2], sv[st * 2 + 1], col, quad,
+                                     none, pr);
+          h8 ph[RT];
+          scale_probs<RT>(pr, sv[st * 2] * s.vinv, sv[st * 2 + 1] * s.vinv,
+                          ts + 32 > lim_lo || ts + 32 > e8, ph);
+#pragma unroll
+          for (int c = 0; c < CT; ++c) {
+            const h8 vf = *reinterpret_cast<const h8*>(buf + kKeys + (st * CT + c) * kFrag + lane * 16);
+#pragma unroll
+            for (int r = 0; r < RT; ++r) s.o[r][c] = mfma_f16(vf, ph[r], s.o[r][c]);
+          }
+        }
+        __syncthreads();
+      }
+      if (full < t1 && sees > full)
+        unfinished_block<D, RT, false>(p, s, b, g, ctx, min(ctx, sees), full, 32, row0, lim, lim_lo, none,
+                                       fresh(lane));
+
+      const int64_t slot0 = ((int64_t)(range + b) * p.c.n_kv + g) * p.rows;
+#pragma unroll
+      for (int r = 0; r < RT; ++r) {
+        const int row = row0 + r * 16 + col;
+        const float L = quad_sum(s.l[r]);
+        const float f = L == 0.0f ? 0.0f : 1.0f / L;
+        if (row < p.rows) {
+          if (quad == 0) p.part_ml[slot0 + row] = {s.m[r], L};
+#pragma unroll
+          for (int c = 0; c < CT; ++c) {
+            f4 v = s.o[r][c] * f;
+            v *= s.vref;
+            *reinterpret_cast<f4*>(p.part_o + (slot0 + row) * D + c * 16 + quad * 4) = v;
+          }
+        }
+      }
+    }
+    at = pl.start + units_of(ctx);
+    if (at >= at_end || !find_unit(p, lens, at, lane, &pl)) return;
   }
 }
 
@@ -739,18 +1026,23 @@ __global__ __launch_bounds__(256) void dense_combine_kernel(const DenseAttnParam
   }
 }
 
-template <int D, bool E4M3, int RT>
+template <int D, bool E4M3, int RT, int RG>
 void launch_split(const DenseAttnParams& p, hipStream_t st) {
-  const dim3 grid(p.ranges, p.c.n_kv, (p.rows + 16 * RT - 1) / (16 * RT));
-  if (p.weights) hipLaunchKernelGGL((dense_split_kernel<D, E4M3, RT, true>), grid, dim3(256), 0, st, p);
-  else hipLaunchKernelGGL((dense_split_kernel<D, E4M3, RT, false>), grid, dim3(256), 0, st, p);
+  const dim3 grid(p.ranges, p.c.n_kv);
+  if (p.weights) hipLaunchKernelGGL((dense_split_kernel<D, E4M3, RT, RG, true>), grid, dim3(256), 0, st, p);
+  else hipLaunchKernelGGL((dense_split_kernel<D, E4M3, RT, RG, false>), grid, dim3(256), 0, st, p);
 }
 
 template <int D, bool E4M3>
 void launch_rows(const DenseAttnParams& p, hipStream_t st) {
-  if (p.rows <= 16) launch_split<D, E4M3, 1>(p, st);
-  else if (p.rows <= 32) launch_split<D, E4M3, 2>(p, st);
-  else launch_split<D, E4M3, 4>(p, st);
+  if (p.rows <= 16) launch_split<D, E4M3, 1, 1>(p, st);
+  else if (p.rows <= 32) launch_split<D, E4M3, 2, 1>(p, st);
+  else if (p.rows <= kSplitRows) launch_split<D, E4M3, 2, 2>(p, st);
+  else {
+    const int tiles = (p.rows + kChunkRows - 1) / kChunkRows;
+    const int pairs = (p.ranges * p.c.n_kv + 7) / 8 * 8;
+    hipLaunchKernelGGL((dense_chunk_kernel<D, E4M3>), dim3(pairs * tiles), dim3(256), 0, st, p);
+  }
 }
 
 }  // namespace

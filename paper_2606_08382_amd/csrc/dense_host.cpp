@@ -356,7 +356,8 @@ starkv_status starkv_dense_read(const starkv_dense_plan* P, const void* cache,
 // Ranges of a split pass over `rows` query rows per KV head: they bring the launch to kSplitTarget
 // workgroups.
 static int64_t split_ranges(const starkv_dense_plan* P, int64_t rows) {
-  const int64_t per_range = P->cfg.n_kv_heads * ((rows + 63) / 64);
+  const int64_t tiles = rows <= kSplitRows ? 1 : (rows + kChunkRows - 1) / kChunkRows;
+  const int64_t per_range = P->cfg.n_kv_heads * tiles;
   return (kSplitTarget + per_range - 1) / per_range;
 }
 
@@ -385,10 +386,11 @@ size_t starkv_dense_workspace_bytes(const starkv_dense_plan* P, int32_t n_q, int
   // Fewer query tokens may take more ranges: the largest need lies at n_q or just before a step
   // of the row tiles.
   const int G = P->cfg.n_q_heads / P->cfg.n_kv_heads;
-  const int gather = with_weights ? std::min(n_q, std::max(64 / G, 1)) : 0;
+  const int gather = with_weights ? std::min(n_q, std::max(kSplitRows / G, 1)) : 0;
   int64_t need = workspace_of(P, n_q, max_ctx, false).total;
-  for (int64_t tiles = 1; tiles <= kSplitTarget; ++tiles) {
-    const int64_t n = 64 * tiles / G;
+  for (int64_t rows = kSplitRows; rows <= (int64_t)kSplitTarget * kChunkRows;
+       rows += rows < kChunkRows ? kChunkRows - rows : kChunkRows) {
+    const int64_t n = rows / G;
     if (n >= n_q) break;
     if (n >= 1) need = std::max(need, workspace_of(P, (int32_t)n, max_ctx, false).total);
   }
@@ -411,8 +413,8 @@ starkv_status starkv_dense_attn(const starkv_dense_plan* P, const void* cache, c
   if (!q || !ctx_len_dev || !out) return fail_with(STARKV_ERR_INVALID_ARG, "NULL device pointer");
   const int G = c.n_q_heads / c.n_kv_heads;
   if (n_q > kMaxDenseCtx) return fail_with(STARKV_ERR_UNSUPPORTED, "n_q %d > %d", n_q, kMaxDenseCtx);
-  if (weights && (int64_t)n_q * G > 64)
-    return fail_with(STARKV_ERR_UNSUPPORTED, "weights with %d query rows per KV head > 64", n_q * G);
+  if (weights && (int64_t)n_q * G > kSplitRows)
+    return fail_with(STARKV_ERR_UNSUPPORTED, "weights with %d query rows per KV head > %d", n_q * G, kSplitRows);
   if (misaligned(q, 2) || misaligned(out, 2)) return fail_with(STARKV_ERR_ALIGNMENT, "q or out not 2-byte aligned");
   if (misaligned(ctx_len_dev, 4) || misaligned(q_len_dev, 4) || misaligned(weights, 4))
     return fail_with(STARKV_ERR_ALIGNMENT, "lengths or weights not 4-byte aligned");

@@ -151,46 +151,68 @@ class Layer:
 
 # ------------------------------------------------------------------- uncompressed layers
 
-_TORCH_DT = {S.DT_F16: "float16", S.DT_BF16: "bfloat16", S.DT_F32: "float32"}
+_types = {}              # library dtype -> the torch types that may hold it
+
+
+def _types_of(dtype):
+    """The torch type of a library dtype and the integer of the same width, for bit patterns."""
+    if not _types:
+        import torch
+        _types.update({S.DT_F16: (torch.float16, torch.int16),
+                       S.DT_BF16: (torch.bfloat16, torch.int16),
+                       S.DT_F32: (torch.float32, torch.int32)})
+    return _types[dtype]
 
 
 def _array(name, t, shape, dtype, device):
-    """Checks a [B][n][H][d] array (its type may also be the integer of the same width, for bit
-    patterns); returns its strides for the library."""
-    import torch
-    own = getattr(torch, _TORCH_DT[dtype])
-    bits = torch.int32 if dtype == S.DT_F32 else torch.int16
-    if t.dtype is not own and t.dtype is not bits:
-        raise TypeError(f"{name}: {t.dtype}, expected {own}")
+    """Checks a [B][n][H][d] array; returns its strides for the library (None: packed)."""
+    if t.dtype not in _types_of(dtype):
+        raise TypeError(f"{name}: {t.dtype}, expected {_types_of(dtype)[0]}")
     if t.device != device:
         raise ValueError(f"{name} is on {t.device}, the layer on {device}")
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if t.is_contiguous():
+        return None
     b, n, h, d = t.stride()
-    if d != 1 and t.shape[3] > 1:
+    if d != 1 and shape[3] > 1:
         raise ValueError(f"{name}: channels must be contiguous")
     return S.starkv_strides(b, n, h)
 
 
 def _vector(name, t, shape, dtype, device):
-    """Checks a packed array of int32 or float32."""
-    import torch
-    if t.dtype is not getattr(torch, dtype):
+    """Checks a packed array of int32 (dtype "int32") or float32."""
+    if str(t.dtype) != "torch." + dtype:
         raise TypeError(f"{name}: {t.dtype}, expected {dtype}")
     if t.device != device:
         raise ValueError(f"{name} is on {t.device}, the layer on {device}")
-    if tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+    if t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name}: expected a contiguous array of shape {tuple(shape)}")
 
 
-def _on(device, stream):
-    """(context of the call's device, its stream): torch's current stream there by default."""
-    import contextlib
-    import torch
-    if stream is None:
-        stream = torch.cuda.current_stream(device).cuda_stream
-    same = torch.cuda.current_device() == device.index
-    return contextlib.nullcontext() if same else torch.cuda.device(device), stream
+class _On:
+    """Makes the arrays' device current for a call; yields the given stream, or torch's current
+    one on that device (its handle alone: the stream object would cost 2 us a call)."""
+
+    __slots__ = ("stream", "other")
+
+    def __init__(self, device, stream):
+        import torch
+        if stream is None:
+            stream = torch._C._cuda_getCurrentRawStream(device.index)
+        self.stream = stream
+        self.other = None
+        if torch.cuda.current_device() != device.index:
+            self.other = torch.cuda.device(device)
+
+    def __enter__(self):
+        if self.other is not None:
+            self.other.__enter__()
+        return self.stream
+
+    def __exit__(self, *exc):
+        if self.other is not None:
+            self.other.__exit__(*exc)
 
 
 def _cuda(device):
@@ -228,8 +250,7 @@ class Rope:
         _vector("positions", pos, shape[:2], "int32", x.device)
         if 0 in shape:
             return out
-        ctx, stream = _on(x.device, stream)
-        with ctx:
+        with _On(x.device, stream) as stream:
             S.starkv_rope(self.plan, a, xs, o, os_, pos, shape[0], shape[1], shape[2],
                           int(inverse), stream=stream)
         return out
@@ -288,8 +309,7 @@ class DenseLayer:
             self._lengths("n_new", n_new)
         if shape[1] == 0:
             return
-        ctx, stream = _on(self.device, stream)
-        with ctx:
+        with _On(self.device, stream) as stream:
             S.starkv_dense_append(self.plan, self.cache, k, ks, v, vs, pos, shape[1], n_new,
                                   stream=stream)
 
@@ -307,8 +327,7 @@ class DenseLayer:
         self._lengths("start", start)
         if shape[1] == 0:
             return
-        ctx, stream = _on(self.device, stream)
-        with ctx:
+        with _On(self.device, stream) as stream:
             S.starkv_dense_read(self.plan, self.cache, ctx_len, start, shape[1], k_out, ks, v_out,
                                 vs, dtype, stream=stream)
 
@@ -344,8 +363,7 @@ class DenseLayer:
             return out
         if ws is None:
             ws = self.workspace(shape[1], weights is not None)
-        ctx, stream = _on(self.device, stream)
-        with ctx:
+        with _On(self.device, stream) as stream:
             S.starkv_dense_attn(self.plan, self.cache, a, qs, shape[1], q_len, ctx_len,
                                 self.capacity if max_ctx is None else max_ctx, o, os_, weights,
                                 ws, stream=stream)
@@ -365,8 +383,7 @@ class DenseLayer:
             _vector("weights_out", weights_out, shape, "float32", self.device)
         if ctx_out is not None:
             self._lengths("ctx_out", ctx_out)
-        ctx, stream = _on(self.device, stream)
-        with ctx:
+        with _On(self.device, stream) as stream:
             S.starkv_dense_evict(self.plan, weights, ctx_len, keep, sink, recent, table_out,
                                  weights_out, ctx_out, stream=stream)
         return (self.table if table_out is None else table_out,

@@ -553,6 +553,36 @@ def test_nonfinite_blocks_reach_only_what_attends_to_them():
                 assert ((got[j, h] - ref[0, j, h]).abs() <= tol[0, j, h]).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("n", [6, 90])
+def test_nonfinite_tokens_of_the_unfinished_block(dtype, n):
+    """Rows before the token are untouched; rows that see it get NaN in the value's channel, or
+    in all of them where the key is not finite."""
+    T, ctx = 128, 128 + 100
+    k, v = kv(1, ctx, 1, 128, dtype)
+    at_v, at_k = ctx - 4, ctx - 2
+    v[0, at_v, 0, 77], v[0, at_v, 0, 3] = math.inf, math.nan
+    k[0, at_k, 0, 5] = math.nan
+    layer = layer_of(1, 2, 1, 128, ctx, 0, T, dtype)
+    layer.append(k.cuda(), v.cuda(), ints([0]))
+    q = rand(1, n, 2, 128, seed=3, dtype=TT[dtype])
+    got = layer.attend(q.cuda(), ints([ctx])).double().cpu()[0]
+    clean_k, clean_v = k.clone(), v.clone()
+    clean_v[0, at_v, 0, 77] = clean_v[0, at_v, 0, 3] = clean_k[0, at_k, 0, 5] = 0
+    ref, tol, _ = reference(clean_k, clean_v, q, [ctx], [n], 0, T)
+    for j in range(n):
+        pos = ctx - n + j
+        nan = torch.isnan(got[j])
+        if pos >= at_k:
+            assert nan.all(), j
+            continue
+        hit = torch.zeros(128, dtype=torch.bool)
+        hit[[3, 77]] = pos >= at_v
+        assert torch.equal(nan, hit.expand(2, 128)), j
+        err = torch.where(hit, 0.0, (got[j] - ref[0, j]).abs())
+        assert (err <= tol[0, j]).all(), j
+
+
 def test_attend_strides():
     layer, k, v, q, out = run_attend([200, 90], n=3, n_q=4, n_kv=2)
     ctx = ints([200, 90])
