@@ -705,6 +705,22 @@ __global__ __launch_bounds__(256, 2) void dense_split_kernel(const DenseAttnPara
   }
 }
 
+// Four channels of an output row.
+__device__ __forceinline__ void store_out(uint16_t* to, f4 v, int bf16, int wide) {
+  union { _Float16 h[4]; __bf16 b[4]; uint16_t u[4]; u2 w; } x;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if (bf16) x.b[e] = (__bf16)v[e];
+    else x.h[e] = (_Float16)v[e];
+  }
+  if (wide) {
+    *reinterpret_cast<u2*>(to) = x.w;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) to[e] = x.u[e];
+  }
+}
+
 // ---- chunk --------------------------------------------------------------------------
 // More than 64 query rows of a KV head: the matrix products bound it (4 d flops per row and token
 // against 2 d bytes per token).  A workgroup takes 128 rows, 32 a wave, so that a wave's state
@@ -898,13 +914,25 @@ __global__ __launch_bounds__(256, 2) void dense_chunk_kernel(const DenseAttnPara
         unfinished_block<D, RT, false>(p, s, b, g, ctx, min(ctx, sees), full, 32, row0, lim, lim_lo, none,
                                        fresh(lane));
 
+      // one range: the whole sequence was seen, and this is the output; else a partial
       const int64_t slot0 = ((int64_t)(range + b) * p.c.n_kv + g) * p.rows;
 #pragma unroll
       for (int r = 0; r < RT; ++r) {
         const int row = row0 + r * 16 + col;
         const float L = quad_sum(s.l[r]);
         const float f = L == 0.0f ? 0.0f : 1.0f / L;
-        if (row < p.rows) {
+        if (p.ranges == 1) {
+          if (lm[r] >= 0) {
+            const int jq = row / p.group, iq = row % p.group;
+            uint16_t* out = p.out + b * p.os_b + jq * p.os_t + (g * p.group + iq) * p.os_h + quad * 4;
+#pragma unroll
+            for (int c = 0; c < CT; ++c) {
+              f4 v = s.o[r][c] * f;
+              v *= s.vref;
+              store_out(out + c * 16, v, p.c.bf16, p.out_wide);
+            }
+          }
+        } else if (row < p.rows) {
           if (quad == 0) p.part_ml[slot0 + row] = {s.m[r], L};
 #pragma unroll
           for (int c = 0; c < CT; ++c) {
@@ -1026,6 +1054,54 @@ __global__ __launch_bounds__(256) void dense_combine_kernel(const DenseAttnParam
   }
 }
 
+// The same for the chunk kernel's many rows and few parts: a wave takes four rows at once.  With one
+// range the rows are written already, but for sequences without tokens.
+template <int D>
+__global__ __launch_bounds__(256) void dense_combine_rows_kernel(const DenseAttnParams p) {
+  constexpr int C = D / 64, K = 4;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int g = blockIdx.y, b = blockIdx.z, row0 = (blockIdx.x * 4 + wave) * K;
+  int first, count, ctx;
+  slots_of(p, b, lane, &first, &count, &ctx);
+  if ((p.ranges == 1 && count > 0) || row0 >= p.rows) return;
+  const int n = min(K, p.rows - row0);
+  const int64_t step = (int64_t)p.c.n_kv * p.rows;
+  const int64_t slot0 = ((int64_t)first * p.c.n_kv + g) * p.rows + row0;
+  float m[K], l[K] = {}, o[K][C] = {};
+#pragma unroll
+  for (int r = 0; r < K; ++r) m[r] = -__builtin_inff();
+  for (int i = 0; i < count; ++i)
+#pragma unroll
+    for (int r = 0; r < K; ++r) m[r] = fmaxf(m[r], p.part_ml[slot0 + i * step + min(r, n - 1)].x);
+#pragma unroll 2
+  for (int i = 0; i < count; ++i)
+#pragma unroll
+    for (int r = 0; r < K; ++r) {
+      const int64_t slot = slot0 + i * step + min(r, n - 1);
+      const Pair ml = p.part_ml[slot];
+      const float f = ml.x == m[r] ? ml.y : ml.y * exp2_fast(ml.x - m[r]);
+      l[r] += f;
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        const float v = p.part_o[slot * D + lane * C + c];
+        o[r][c] += f == 0.0f ? 0.0f : f * v;
+      }
+    }
+#pragma unroll
+  for (int r = 0; r < K; ++r) {
+    const int row = row0 + r;
+    if (row_limit(p, b, ctx, row) < 0) continue;
+    const int jq = row / p.group, iq = row % p.group;
+    uint16_t* out = p.out + b * p.os_b + jq * p.os_t + (g * p.group + iq) * p.os_h + lane * C;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const float v = l[r] == 0.0f ? 0.0f : o[r][c] / l[r];
+      out[c] = p.c.bf16 ? __builtin_bit_cast(uint16_t, (__bf16)v)
+                        : __builtin_bit_cast(uint16_t, (_Float16)v);
+    }
+  }
+}
+
 template <int D, bool E4M3, int RT, int RG>
 void launch_split(const DenseAttnParams& p, hipStream_t st) {
   const dim3 grid(p.ranges, p.c.n_kv);
@@ -1058,6 +1134,12 @@ int launch_dense_attn(const DenseAttnParams& p, void* stream) {
   }
   int e = (int)hipGetLastError();
   if (e) return e;
+  if (p.rows > kSplitRows) {
+    const dim3 grid((p.rows + 15) / 16, p.c.n_kv, p.c.batch);
+    if (p.c.d == 128) hipLaunchKernelGGL(dense_combine_rows_kernel<128>, grid, dim3(256), 0, st, p);
+    else hipLaunchKernelGGL(dense_combine_rows_kernel<64>, grid, dim3(256), 0, st, p);
+    return (int)hipGetLastError();
+  }
   const int J = (p.max_ctx + (1 << p.c.shift) - 1) >> p.c.shift;
   const dim3 grid(p.rows + (p.weights ? (J + 255) / 256 : 0), p.c.n_kv, p.c.batch);
   if (p.c.d == 128) hipLaunchKernelGGL(dense_combine_kernel<128>, grid, dim3(256), 0, st, p);

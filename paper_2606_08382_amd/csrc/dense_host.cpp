@@ -51,10 +51,10 @@ bool rows_apart(const starkv_strides& s, int64_t B, int64_t n, int64_t heads, in
          (heads <= 1 || std::llabs(s.head) >= d);
 }
 
-// Whether every row of the array starts on a multiple of 16 bytes.
-bool rows_wide(const void* p, const starkv_strides& s, int64_t elem) {
-  return !misaligned(p, 16) && s.batch * elem % 16 == 0 && s.token * elem % 16 == 0 &&
-         s.head * elem % 16 == 0;
+// Whether every row of the array starts on a multiple of `bytes`.
+bool rows_wide(const void* p, const starkv_strides& s, int64_t elem, int bytes = 16) {
+  return !misaligned(p, bytes) && s.batch * elem % bytes == 0 && s.token * elem % bytes == 0 &&
+         s.head * elem % bytes == 0;
 }
 
 bool is_dtype16(int dt) { return dt == STARKV_DT_F16 || dt == STARKV_DT_BF16; }
@@ -372,7 +372,9 @@ static DenseWorkspace workspace_of(const starkv_dense_plan* P, int32_t n_q, int3
   const starkv_dense_config& c = P->cfg;
   const int64_t rows = (int64_t)n_q * (c.n_q_heads / c.n_kv_heads);
   w.ranges = split_ranges(P, rows);
-  const int64_t slots = (w.ranges + c.batch) * c.n_kv_heads * rows;
+  // (the chunk kernel writes the output itself where one range holds all sequences)
+  const bool whole = rows > kSplitRows && w.ranges == 1;
+  const int64_t slots = whole ? 1 : (w.ranges + c.batch) * c.n_kv_heads * rows;
   w.ml = align256(slots * c.head_dim * 4);
   w.sub = w.ml + align256(slots * 8);
   w.sub_per_head = (max_ctx + 15) / 16;
@@ -451,6 +453,7 @@ starkv_status starkv_dense_attn(const starkv_dense_plan* P, const void* cache, c
   p.ranges = (int32_t)w.ranges;
   p.sub_per_head = w.sub_per_head;
   p.q_wide = rows_wide(q, a, 2);
+  p.out_wide = rows_wide(out, o, 2, 8);
   p.scale_log2 = (float)(P->scale * 1.4426950408889634);
   return hip_status(launch_dense_attn(p, static_cast<void*>(stream)), "dense attention launch");
 }

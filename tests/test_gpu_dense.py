@@ -486,6 +486,17 @@ def test_several_query_tokens(n, n_q, n_kv, T, code, dtype, d):
                q_len=[n, 0, n - 1, 1])
 
 
+def test_many_query_rows_need_no_partials():
+    """Enough row tiles to fill the device: outputs are written in one pass; empty and padded
+    sequences, rows that are not 8-byte aligned."""
+    n, ctx = 600, [700, 0, 650]
+    run_attend(ctx, n=n, n_q=48, n_kv=16, d=64, T=16, q_len=[n, n, 77])
+    layer, k, v, q, out = run_attend([640, 600], n=600, n_q=48, n_kv=16, d=64, T=32, code=1)
+    odd = torch.full((2, 600, 48, 65), 3.0, dtype=torch.bfloat16, device="cuda")
+    layer.attend(q.cuda(), ints([640, 600]), out=odd[..., 1:])
+    assert torch.equal(odd[..., 1:], out) and (odd[..., 0] == 3).all()
+
+
 def test_large_scores_and_scales():
     run_attend([700, 130], k_scale=40.0)                     # one token takes nearly all
     run_attend([700, 130], k_scale=3000.0, dtype="bf16", code=1)
