@@ -39,7 +39,7 @@ constexpr int kWavesA = 4;
 constexpr int kUnit = 32 * kWavesA;         // tokens of a workgroup's round: granule of ranges
 constexpr float kBelow = 6.0f;              // reference: largest score - kBelow (log2)
 constexpr float kAbove = 14.0f;             // scores may pass the reference by this much
-constexpr float kTinyScale = 0x1p-100f;     // smallest reference of the value scales
+constexpr float kTinyScale = -100.0f;       // smallest reference of the value scales (log2)
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -88,6 +88,11 @@ __device__ __forceinline__ h8 code8(uint32_t lo, uint32_t hi) {
   code4<E4M3>(lo, u.p);
   code4<E4M3>(hi, u.p + 2);
   return u.v;
+}
+
+__device__ __forceinline__ int fresh(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
 }
 
 __device__ __forceinline__ f4 mfma_f16(h8 a, h8 b, f4 c) {
@@ -194,18 +199,13 @@ __device__ __forceinline__ int row_limit(const DenseAttnParams& p, int b, int ct
   return max(ctx - q_len + j + 1, 0);
 }
 
-__device__ __forceinline__ int fresh(int x) {
-  asm volatile("" : "+v"(x));
-  return x;
-}
-
 // ---- split --------------------------------------------------------------------------
 
 template <int D>
 struct Tile {                       // codes of a 32-token step: two subtiles
   static constexpr int N = D / 64;
   u4 k[2][N], v[2][N];
-  float sk[2], sv[2];
+  float sk[2], lsv[2];
 };
 
 // State of RT tiles of 16 query rows.
@@ -213,18 +213,14 @@ template <int D, int RT>
 struct State {
   f4 o[RT][D / 16];
   float m[RT], l[RT];               // reference (log2) of a lane's column; its lane's sum
-  float vref, vinv;                 // reference of the value scales and its inverse
+  float lv;                         // reference of the value scales (log2)
 };
 
-// Raises references so that scores up to `top` and value scales up to sv fit.
+// Raises references so that scores up to `top` and (log2) value scales up to lsv fit.
 template <int D, int RT>
-__device__ __forceinline__ void raise(State<D, RT>& s, const float* top, float sv) {
-  float vr = 1.0f;
-  if (sv > s.vref) {
-    vr = s.vref / sv;
-    s.vref = sv;
-    s.vinv = 1.0f / sv;
-  }
+__device__ __forceinline__ void raise(State<D, RT>& s, const float* top, float lsv) {
+  const float lv = fmaxf(s.lv, lsv), vr = exp2_fast(s.lv - lv);
+  s.lv = lv;
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
     const float t = quad_max(top[r]);
@@ -238,75 +234,117 @@ __device__ __forceinline__ void raise(State<D, RT>& s, const float* top, float s
   }
 }
 
+template <int D, int RT>
+__device__ __forceinline__ void reset(State<D, RT>& s) {
+#pragma unroll
+  for (int r = 0; r < RT; ++r) {
+    s.m[r] = -__builtin_inff();
+    s.l[r] = 0.0f;
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c) s.o[r][c] = (f4){0.0f, 0.0f, 0.0f, 0.0f};
+  }
+  s.lv = kTinyScale;
+}
+
 // Where a split pass with weights leaves the sums of 16-token subtiles.
 struct SubSums {
   Pair* at;                         // of the KV head's first subtile, row 0
   int row0, rows;                   // the wave's first row; rows of the KV head
 };
 
-// Probabilities pr of a 32-token step of tokens t.. from its log2 scores x (tokens from lim[] on,
-// and from `end` on, are absent), added to the running sums; sv: value scales of its subtiles.
-// A lane's tokens are t + 16 a + 4 quad + e, a = 0, 1, e = 0..3, for column col of each row tile.
+// Probabilities of a 32-token step of tokens t.., each times its subtile's value scale over the
+// wave's reference, as the products' fp16 operand or in fp32; the running sums take them without
+// that factor.  sc: products q.k; fk: what makes them log2 scores; lsv: log2 of the value scales
+// of the two subtiles.  Tokens from lim[] on, and from `end` on, are absent.  A lane's tokens
+// are t + 16 a + 4 quad + e, a = 0, 1, e = 0..3, for column col of each row tile.
+//
+// The factor enters the exponent, 2^(x - m + d) with d = lsv - reference, instead of a product per
+// probability; d is held above -40, where fp16 has dropped the values anyway, so that the sums
+// keep every token.
 template <int D, int RT, bool SUMS>
-__device__ __forceinline__ void softmax_step(State<D, RT>& s, f4 (&x)[RT][2], const int (&lim)[RT],
-                                             int lim_lo, int t, int end, float sv0, float sv1,
-                                             int col, int quad, const SubSums& sums,
-                                             float (&pr)[RT][8]) {
-  if (t + 32 > lim_lo || t + 32 > end) {
+__device__ __forceinline__ void softmax_step(State<D, RT>& s, f4 (&sc)[RT][2], float (&fk)[RT][2],
+                                             const int (&lim)[RT], int lim_lo, int t, int end,
+                                             float lsv0, float lsv1, int col, int quad,
+                                             const SubSums& sums, float (&pr)[RT][8]) {
+  const bool masked = t + 32 > lim_lo || t + 32 > end;
+  if (masked) {
+    // (through fresh(), so that the selects stay in the branch)
+    const int first = fresh(t + quad * 4);
 #pragma unroll
     for (int r = 0; r < RT; ++r)
 #pragma unroll
-      for (int a = 0; a < 2; ++a)
+      for (int a = 0; a < 2; ++a) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const int tok = t + a * 16 + quad * 4 + e;
-          x[r][a][e] = tok < lim[r] && tok < end ? x[r][a][e] : -__builtin_inff();
+          const int tok = first + a * 16 + e;
+          sc[r][a][e] = tok < lim[r] && tok < end ? sc[r][a][e] * fk[r][a] : -__builtin_inff();
         }
+        fk[r][a] = 1.0f;
+      }
   }
   float top[RT];
-  bool over = fmaxf(sv0, sv1) > s.vref;
+  const float lsv = fmaxf(lsv0, lsv1);
+  bool over = lsv > s.lv;
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
-    top[r] = fmaxf(fmaxf(fmaxf(x[r][0][0], x[r][0][1]), fmaxf(x[r][0][2], x[r][0][3])),
-                   fmaxf(fmaxf(x[r][1][0], x[r][1][1]), fmaxf(x[r][1][2], x[r][1][3])));
+    const float x = fmaxf(fmaxf(sc[r][0][0], sc[r][0][1]), fmaxf(sc[r][0][2], sc[r][0][3]));
+    const float y = fmaxf(fmaxf(sc[r][1][0], sc[r][1][1]), fmaxf(sc[r][1][2], sc[r][1][3]));
+    top[r] = fmaxf(x * fk[r][0], y * fk[r][1]);
     over |= top[r] > s.m[r] + kAbove;
   }
-  if (__any(over)) raise(s, top, fmaxf(sv0, sv1));
+  if (__any(over)) raise(s, top, lsv);
+  // (a NaN scale makes NaN of its tokens' probabilities, and of nothing else)
+  float d[2] = {lsv0 - s.lv, lsv1 - s.lv}, back[2];
+#pragma unroll
+  for (int a = 0; a < 2; ++a) {
+    d[a] = d[a] < -40.0f ? -40.0f : d[a];
+    back[a] = d[a] == d[a] ? exp2_fast(-d[a]) : 1.0f;
+  }
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
     // a column that has seen nothing keeps reference -inf: x - 0 is -inf, its exponential 0
     const float m = s.m[r] == -__builtin_inff() ? 0.0f : s.m[r];
 #pragma unroll
     for (int a = 0; a < 2; ++a) {
+      const float c = d[a] - m;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) pr[r][a * 4 + e] = exp2_fast(x[r][a][e] - m);
+      for (int e = 0; e < 4; ++e) pr[r][a * 4 + e] = exp2_fast(__builtin_fmaf(sc[r][a][e], fk[r][a], c));
+    }
+  }
+  if (masked) {
+    const float absent = __int_as_float(fresh(0xff800000));
+    // an absent token's probability is zero whatever its block's scale
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) pr[r][i] = sc[r][i >> 2][i & 3] == absent ? 0.0f : pr[r][i];
+  }
+#pragma unroll
+  for (int r = 0; r < RT; ++r)
+#pragma unroll
+    for (int a = 0; a < 2; ++a) {
       const float part = (pr[r][a * 4] + pr[r][a * 4 + 1]) + (pr[r][a * 4 + 2] + pr[r][a * 4 + 3]);
-      s.l[r] += part;
+      s.l[r] = __builtin_fmaf(part, back[a], s.l[r]);
       if constexpr (SUMS) {
-        const float y = quad_sum(part);
+        const float y = quad_sum(part) * back[a];
         const int row = sums.row0 + r * 16 + col;
         if (quad == 0 && row < sums.rows && t + a * 16 < end)
           sums.at[(int64_t)((t >> 4) + a) * sums.rows + row] = {y, s.m[r]};
       }
     }
-  }
 }
 
-// Probabilities of a step of finished blocks as the products' fp16 operand.
 template <int RT>
-__device__ __forceinline__ void scale_probs(const float (&pr)[RT][8], float f0, float f1, bool masked,
-                                            h8 (&ph)[RT]) {
+__device__ __forceinline__ void to_operand(const float (&pr)[RT][8], h8 (&ph)[RT]) {
 #pragma unroll
   for (int r = 0; r < RT; ++r)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) ph[r][e] = (_Float16)(pr[r][e] * (e < 4 ? f0 : f1));
-  if (masked) {
-    // an absent token's probability is zero whatever its block's scale
-#pragma unroll
-    for (int r = 0; r < RT; ++r)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) ph[r][e] = pr[r][e] == 0.0f ? (_Float16)0.0f : ph[r][e];
-  }
+    for (int e = 0; e < 8; ++e) ph[r][e] = (_Float16)pr[r][e];
+}
+
+// log2 of a block's value scale (of a block of zeros: the smallest reference; NaN stays).
+__device__ __forceinline__ float log_scale(float sv) {
+  return sv < 0x1p-100f ? kTinyScale : __builtin_amdgcn_logf(sv);
 }
 
 // Query rows row0 + 16 r + col, channels i*64 + quad*16 + h*8 + e (operand n = 2 i + h), as given.
@@ -399,13 +437,11 @@ __device__ __forceinline__ void unfinished_block(const DenseAttnParams& p, State
         for (int a = 0; a < 2; ++a) sc[r][a] = mfma_raw(k[a], q, sc[r][a], bf16);
       }
     }
+    float fk[RT][2];
 #pragma unroll
-    for (int r = 0; r < RT; ++r) {
-      sc[r][0] *= p.scale_log2;
-      sc[r][1] *= p.scale_log2;
-    }
+    for (int r = 0; r < RT; ++r) fk[r][0] = fk[r][1] = p.scale_log2;
     float pr[RT][8];
-    softmax_step<D, RT, SUMS>(s, sc, lim, lim_lo, t, ctx, 1.0f, 1.0f, col, quad, sums, pr);
+    softmax_step<D, RT, SUMS>(s, sc, fk, lim, lim_lo, t, ctx, 0.0f, 0.0f, col, quad, sums, pr);
     u4 pa[RT], pb[RT];                              // fp16; or two bf16 parts
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
@@ -413,7 +449,7 @@ __device__ __forceinline__ void unfinished_block(const DenseAttnParams& p, State
       lo.v = (u4){0, 0, 0, 0};
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float x = pr[r][e] * s.vinv;
+        const float x = pr[r][e];
         if (bf16) {
           hi.b[e] = (__bf16)x;
           lo.b[e] = (__bf16)(x - (float)hi.b[e]);
@@ -545,12 +581,12 @@ __global__ __launch_bounds__(256, 2) void dense_split_kernel(const DenseAttnPara
   lim_lo = __builtin_amdgcn_readfirstlane(lim_lo);
 
   const int steps = e8 > tw ? (e8 - tw + kRound - 1) / kRound : 0;
-  struct Entry { uint32_t sub; float sk, sv; };
+  struct Entry { uint32_t sub; float sk, lsv; };
   auto entry_of = [&](int e, int i0) {
     const int t = entry_token(i0);
     e = min(max(e, 0), p.c.n_blocks - 1);
     const Pair sc = p.c.scales[e];
-    return Entry{((uint32_t)e << (sh - 3)) + ((uint32_t)(t & (T - 1)) >> 4), sc.x, sc.y};
+    return Entry{((uint32_t)e << (sh - 3)) + ((uint32_t)(t & (T - 1)) >> 4), sc.x, log_scale(sc.y)};
   };
   const uint32_t v_sub = (uint32_t)T >> 4;          // from a key subtile to its value subtile
   auto load = [&](Tile<D>& x, const Entry& en, int i) {
@@ -559,7 +595,7 @@ __global__ __launch_bounds__(256, 2) void dense_split_kernel(const DenseAttnPara
       const int l = 2 * (i & 31) + a;
       const uint32_t sub = __builtin_amdgcn_readlane(en.sub, l);
       x.sk[a] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(en.sk), l));
-      x.sv[a] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(en.sv), l));
+      x.lsv[a] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(en.lsv), l));
       const uint8_t* kb = p.c.codes + (uint64_t)sub * (16 * D) + lane * 16;
       const uint8_t* vb = p.c.codes + (uint64_t)(sub + v_sub) * (16 * D) + lane * 16;
       // (streaming: a code is read once a step; 5.8 TB/s with plain loads, 6.7 with these)
@@ -592,21 +628,13 @@ __global__ __launch_bounds__(256, 2) void dense_split_kernel(const DenseAttnPara
   scale_queries<D, RT>(p, raw, q, qs);
 
   State<D, RT> s;
-#pragma unroll
-  for (int r = 0; r < RT; ++r) {
-    s.m[r] = -__builtin_inff();
-    s.l[r] = 0.0f;
-#pragma unroll
-    for (int c = 0; c < CT; ++c) s.o[r][c] = (f4){0.0f, 0.0f, 0.0f, 0.0f};
-  }
-  s.vref = kTinyScale;
-  s.vinv = 1.0f / kTinyScale;
-
+  reset(s);
   const SubSums sums = {SUMS ? p.sub + head * p.sub_per_head * p.rows : nullptr, row0, p.rows};
   // ---- finished blocks
   auto compute = [&](const Tile<D>& y, int i) {
     const int t = tw + i * kRound;
     f4 sc[RT][2];
+    float fk[RT][2];
 #pragma unroll
     for (int a = 0; a < 2; ++a) {
 #pragma unroll
@@ -620,12 +648,12 @@ __global__ __launch_bounds__(256, 2) void dense_split_kernel(const DenseAttnPara
           for (int r = 0; r < RT; ++r) sc[r][a] = mfma_f16(k, q[r][2 * n + h], sc[r][a]);
         }
 #pragma unroll
-      for (int r = 0; r < RT; ++r) sc[r][a] *= y.sk[a] * qs[r];
+      for (int r = 0; r < RT; ++r) fk[r][a] = y.sk[a] * qs[r];
     }
     float pr[RT][8];
-    softmax_step<D, RT, SUMS>(s, sc, lim, lim_lo, t, e8, y.sv[0], y.sv[1], col, quad, sums, pr);
+    softmax_step<D, RT, SUMS>(s, sc, fk, lim, lim_lo, t, e8, y.lsv[0], y.lsv[1], col, quad, sums, pr);
     h8 ph[RT];
-    scale_probs<RT>(pr, y.sv[0] * s.vinv, y.sv[1] * s.vinv, t + 32 > lim_lo || t + 32 > e8, ph);
+    to_operand<RT>(pr, ph);
 #pragma unroll
     for (int n = 0; n < N; ++n)
 #pragma unroll
@@ -663,6 +691,7 @@ __global__ __launch_bounds__(256, 2) void dense_split_kernel(const DenseAttnPara
   }
   __syncthreads();
   const int64_t slot0 = ((int64_t)(blockIdx.x + it.b) * p.c.n_kv + g) * p.rows;
+  const float vref = exp2_fast(s.lv);
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
     const int group = wave % RG;
@@ -684,7 +713,7 @@ __global__ __launch_bounds__(256, 2) void dense_split_kernel(const DenseAttnPara
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
       f4 v = s.o[r][c] * f;                         // at most the largest code, then the scale
-      v *= s.vref;
+      v *= vref;
       *reinterpret_cast<f4*>(&so[wave][col][c * 16 + quad * 4]) = v;
     }
     __syncthreads();
@@ -786,27 +815,19 @@ __global__ __launch_bounds__(256, 2) void dense_chunk_kernel(const DenseAttnPara
         scale_queries<D, RT>(p, raw, q, qs);
       }
       State<D, RT> s;
-#pragma unroll
-      for (int r = 0; r < RT; ++r) {
-        s.m[r] = -__builtin_inff();
-        s.l[r] = 0.0f;
-#pragma unroll
-        for (int c = 0; c < CT; ++c) s.o[r][c] = (f4){0.0f, 0.0f, 0.0f, 0.0f};
-      }
-      s.vref = kTinyScale;
-      s.vinv = 1.0f / kTinyScale;
+      reset(s);
       const SubSums none = {nullptr, 0, 0};
 
       const int e8 = min(min(t1, full), (sees + 15) & ~15);
       const int n = e8 > t0 ? (e8 - t0 + kTile - 1) / kTile : 0;
       const int32_t* table = p.c.table + head * p.c.blocks_per_head;
       // entries of 16 tiles, a subtile per lane
-      struct Entry { uint32_t sub; float sk, sv; };
+      struct Entry { uint32_t sub; float sk, lsv; };
       auto entries = [&](int i0) {
         const int t = max(min(t0 + i0 * kTile + lane * 16, e8 - 16), 0);
         const int e = min(max(table[t >> sh], 0), p.c.n_blocks - 1);
         const Pair sc = p.c.scales[e];
-        return Entry{((uint32_t)e << (sh - 3)) + ((uint32_t)(t & (T - 1)) >> 4), sc.x, sc.y};
+        return Entry{((uint32_t)e << (sh - 3)) + ((uint32_t)(t & (T - 1)) >> 4), sc.x, log_scale(sc.y)};
       };
       const uint32_t v_sub = (uint32_t)T >> 4;
       // A thread's codes of a tile: key units tid + 256 i (subtile, then 16-byte unit); value units of
@@ -862,12 +883,12 @@ __global__ __launch_bounds__(256, 2) void dense_chunk_kernel(const DenseAttnPara
       __syncthreads();
       for (int i = 0; i < n; ++i) {
         // the scales of this tile (its entries may be replaced below)
-        float sk[4], sv[4];
+        float sk[4], lsv[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           const int l = (i & 15) * 4 + k;
           sk[k] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(now.sk), l));
-          sv[k] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(now.sv), l));
+          lsv[k] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(now.lsv), l));
         }
         if (i + 1 < n) store(lds[(i + 1) & 1]);
         if (((i + 1) & 15) == 0) {
@@ -881,6 +902,7 @@ __global__ __launch_bounds__(256, 2) void dense_chunk_kernel(const DenseAttnPara
 #pragma unroll
         for (int st = 0; st < 2; ++st) {
           f4 sc[RT][2];
+          float fk[RT][2];
 #pragma unroll
           for (int a = 0; a < 2; ++a) {
 #pragma unroll
@@ -892,15 +914,13 @@ __global__ __launch_bounds__(256, 2) void dense_chunk_kernel(const DenseAttnPara
               for (int r = 0; r < RT; ++r) sc[r][a] = mfma_f16(kf, q[r][k], sc[r][a]);
             }
 #pragma unroll
-            for (int r = 0; r < RT; ++r) sc[r][a] *= sk[st * 2 + a] * qs[r];
+            for (int r = 0; r < RT; ++r) fk[r][a] = sk[st * 2 + a] * qs[r];
           }
           float pr[RT][8];
-          const int ts = t + st * 32;
-          softmax_step<D, RT, false>(s, sc, lim, lim_lo, ts, e8, sv[st * 2], sv[st * 2 + 1], col, quad,
-                                     none, pr);
+          softmax_step<D, RT, false>(s, sc, fk, lim, lim_lo, t + st * 32, e8, lsv[st * 2],
+                                     lsv[st * 2 + 1], col, quad, none, pr);
           h8 ph[RT];
-          scale_probs<RT>(pr, sv[st * 2] * s.vinv, sv[st * 2 + 1] * s.vinv,
-                          ts + 32 > lim_lo || ts + 32 > e8, ph);
+          to_operand<RT>(pr, ph);
 #pragma unroll
           for (int c = 0; c < CT; ++c) {
             const h8 vf = *reinterpret_cast<const h8*>(buf + kKeys + (st * CT + c) * kFrag + lane * 16);
@@ -914,6 +934,7 @@ __global__ __launch_bounds__(256, 2) void dense_chunk_kernel(const DenseAttnPara
         unfinished_block<D, RT, false>(p, s, b, g, ctx, min(ctx, sees), full, 32, row0, lim, lim_lo, none,
                                        fresh(lane));
 
+      const float vref = exp2_fast(s.lv);
       // one range: the whole sequence was seen, and this is the output; else a partial
       const int64_t slot0 = ((int64_t)(range + b) * p.c.n_kv + g) * p.rows;
 #pragma unroll
@@ -928,7 +949,7 @@ __global__ __launch_bounds__(256, 2) void dense_chunk_kernel(const DenseAttnPara
 #pragma unroll
             for (int c = 0; c < CT; ++c) {
               f4 v = s.o[r][c] * f;
-              v *= s.vref;
+              v *= vref;
               store_out(out + c * 16, v, p.c.bf16, p.out_wide);
             }
           }
@@ -937,7 +958,7 @@ __global__ __launch_bounds__(256, 2) void dense_chunk_kernel(const DenseAttnPara
 #pragma unroll
           for (int c = 0; c < CT; ++c) {
             f4 v = s.o[r][c] * f;
-            v *= s.vref;
+            v *= vref;
             *reinterpret_cast<f4*>(p.part_o + (slot0 + row) * D + c * 16 + quad * 4) = v;
           }
         }

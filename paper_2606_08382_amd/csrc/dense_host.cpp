@@ -353,12 +353,25 @@ starkv_status starkv_dense_read(const starkv_dense_plan* P, const void* cache,
 
 // ----------------------------------------------------------------------------- attention
 
-// Ranges of a split pass over `rows` query rows per KV head: they bring the launch to kSplitTarget
-// workgroups.
+// Ranges of a pass over `rows` query rows per KV head.  Its workgroups (ranges x KV heads x row
+// tiles) run kSplitTarget at a time; the ranges are as many as one round takes, or, where a few
+// more make the last round fuller, up to four more (each range costs 2 % for its prologue and
+// partials).
 static int64_t split_ranges(const starkv_dense_plan* P, int64_t rows) {
   const int64_t tiles = rows <= kSplitRows ? 1 : (rows + kChunkRows - 1) / kChunkRows;
   const int64_t per_range = P->cfg.n_kv_heads * tiles;
-  return (kSplitTarget + per_range - 1) / per_range;
+  const int64_t one = std::max<int64_t>(kSplitTarget / per_range, 1);
+  int64_t best = one;
+  double least = 1e30;
+  for (int64_t r = one; r <= one + 4; ++r) {
+    const double rounds = (double)((r * per_range + kSplitTarget - 1) / kSplitTarget);
+    const double cost = rounds / r * (1.0 + 0.02 * (r - one));
+    if (cost < least) {
+      least = cost;
+      best = r;
+    }
+  }
+  return best;
 }
 
 struct DenseWorkspace {
