@@ -252,54 +252,73 @@ struct SubSums {
   int row0, rows;                   // the wave's first row; rows of the KV head
 };
 
-// Probabilities of a 32-token step of tokens t.., each times its subtile's value scale over the
-// wave's reference, as the products' fp16 operand or in fp32; the running sums take them without
-// that factor.  sc: products q.k; fk: what makes them log2 scores; lsv: log2 of the value scales
-// of the two subtiles.  Tokens from lim[] on, and from `end` on, are absent.  A lane's tokens
-// are t + 16 a + 4 quad + e, a = 0, 1, e = 0..3, for column col of each row tile.
+// Softmax of ST 32-token steps of tokens t.., in two parts.  sc: products q.k; fk: what makes them
+// log2 scores; lsv: log2 of the value scales of the subtiles.  Tokens from lim[] on, and from
+// `end` on, are absent.  A lane's tokens are t + 32 st + 16 a + 4 quad + e, a = 0, 1, e = 0..3, for
+// column col of each row tile.
 //
-// The factor enters the exponent, 2^(x - m + d) with d = lsv - reference, instead of a product per
-// probability; d is held above -40, where fp16 has dropped the values anyway, so that the sums
-// keep every token.
-template <int D, int RT, bool SUMS>
-__device__ __forceinline__ void softmax_step(State<D, RT>& s, f4 (&sc)[RT][2], float (&fk)[RT][2],
-                                             const int (&lim)[RT], int lim_lo, int t, int end,
-                                             float lsv0, float lsv1, int col, int quad,
-                                             const SubSums& sums, float (&pr)[RT][8]) {
-  const bool masked = t + 32 > lim_lo || t + 32 > end;
+// begin_steps masks, raises the references where needed, and leaves d, the log2 of each subtile's
+// value scale over the wave's reference.  finish_step gives a step's probabilities times that
+// factor, as the product with the values takes them, and adds them to the running sums without
+// it.  The factor enters the exponent, 2^(x - m + d), instead of a product per probability; d is
+// held above -40, where fp16 has dropped the values anyway, so that the sums keep every token.
+template <int D, int RT, int ST>
+__device__ __forceinline__ void begin_steps(State<D, RT>& s, f4 (&sc)[ST][RT][2], float (&fk)[ST][RT][2],
+                                            const int (&lim)[RT], int lim_lo, int t, int end,
+                                            const float* lsv, int quad, float (&d)[2 * ST]) {
+  const bool masked = t + 32 * ST > lim_lo || t + 32 * ST > end;
   if (masked) {
     // (through fresh(), so that the selects stay in the branch)
     const int first = fresh(t + quad * 4);
 #pragma unroll
-    for (int r = 0; r < RT; ++r)
+    for (int st = 0; st < ST; ++st)
 #pragma unroll
-      for (int a = 0; a < 2; ++a) {
+      for (int r = 0; r < RT; ++r)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int tok = first + a * 16 + e;
-          sc[r][a][e] = tok < lim[r] && tok < end ? sc[r][a][e] * fk[r][a] : -__builtin_inff();
+        for (int a = 0; a < 2; ++a) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int tok = first + st * 32 + a * 16 + e;
+            // (a NaN scale is moved to the scores of the tokens that are seen)
+            const float x = __builtin_fmaf(sc[st][r][a][e], fk[st][r][a], lsv[st * 2 + a] * 0.0f);
+            sc[st][r][a][e] = tok < lim[r] && tok < end ? x : -__builtin_inff();
+          }
+          fk[st][r][a] = 1.0f;
         }
-        fk[r][a] = 1.0f;
-      }
   }
-  float top[RT];
-  const float lsv = fmaxf(lsv0, lsv1);
-  bool over = lsv > s.lv;
+  float top[RT], most = lsv[0];
+#pragma unroll
+  for (int i = 1; i < 2 * ST; ++i) most = fmaxf(most, lsv[i]);
+  bool over = most > s.lv;
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
-    const float x = fmaxf(fmaxf(sc[r][0][0], sc[r][0][1]), fmaxf(sc[r][0][2], sc[r][0][3]));
-    const float y = fmaxf(fmaxf(sc[r][1][0], sc[r][1][1]), fmaxf(sc[r][1][2], sc[r][1][3]));
-    top[r] = fmaxf(x * fk[r][0], y * fk[r][1]);
+    top[r] = -__builtin_inff();
+#pragma unroll
+    for (int st = 0; st < ST; ++st)
+#pragma unroll
+      for (int a = 0; a < 2; ++a) {
+        const f4 x = sc[st][r][a];
+        top[r] = fmaxf(top[r], fmaxf(fmaxf(fmaxf(x[0], x[1]), x[2]), x[3]) * fk[st][r][a]);
+      }
     over |= top[r] > s.m[r] + kAbove;
   }
-  if (__any(over)) raise(s, top, lsv);
-  // (a NaN scale makes NaN of its tokens' probabilities, and of nothing else)
-  float d[2] = {lsv0 - s.lv, lsv1 - s.lv}, back[2];
+  if (__any(over)) raise(s, top, most);
 #pragma unroll
-  for (int a = 0; a < 2; ++a) {
-    d[a] = d[a] < -40.0f ? -40.0f : d[a];
-    back[a] = d[a] == d[a] ? exp2_fast(-d[a]) : 1.0f;
+  for (int i = 0; i < 2 * ST; ++i) {
+    d[i] = lsv[i] - s.lv;
+    d[i] = d[i] < -40.0f || (masked && d[i] != d[i]) ? -40.0f : d[i];
   }
+}
+
+template <int D, int RT, bool SUMS>
+__device__ __forceinline__ void finish_step(State<D, RT>& s, const f4 (&sc)[RT][2],
+                                            const float (&fk)[RT][2], const float* d, int t, int end,
+                                            int col, int quad, const SubSums& sums,
+                                            float (&pr)[RT][8]) {
+  // (a NaN scale makes NaN of its tokens' probabilities, and of nothing else)
+  float back[2];
+#pragma unroll
+  for (int a = 0; a < 2; ++a) back[a] = d[a] == d[a] ? exp2_fast(-d[a]) : 1.0f;
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
     // a column that has seen nothing keeps reference -inf: x - 0 is -inf, its exponential 0
@@ -309,20 +328,6 @@ __device__ __forceinline__ void softmax_step(State<D, RT>& s, f4 (&sc)[RT][2], f
       const float c = d[a] - m;
 #pragma unroll
       for (int e = 0; e < 4; ++e) pr[r][a * 4 + e] = exp2_fast(__builtin_fmaf(sc[r][a][e], fk[r][a], c));
-    }
-  }
-  if (masked) {
-    const float absent = __int_as_float(fresh(0xff800000));
-    // an absent token's probability is zero whatever its block's scale
-#pragma unroll
-    for (int r = 0; r < RT; ++r)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) pr[r][i] = sc[r][i >> 2][i & 3] == absent ? 0.0f : pr[r][i];
-  }
-#pragma unroll
-  for (int r = 0; r < RT; ++r)
-#pragma unroll
-    for (int a = 0; a < 2; ++a) {
       const float part = (pr[r][a * 4] + pr[r][a * 4 + 1]) + (pr[r][a * 4 + 2] + pr[r][a * 4 + 3]);
       s.l[r] = __builtin_fmaf(part, back[a], s.l[r]);
       if constexpr (SUMS) {
@@ -332,6 +337,7 @@ __device__ __forceinline__ void softmax_step(State<D, RT>& s, f4 (&sc)[RT][2], f
           sums.at[(int64_t)((t >> 4) + a) * sums.rows + row] = {y, s.m[r]};
       }
     }
+  }
 }
 
 template <int RT>
@@ -416,9 +422,9 @@ __device__ __forceinline__ void unfinished_block(const DenseAttnParams& p, State
   const uint16_t* kt = p.c.tails + ((int64_t)b * p.c.n_kv + g) * 2 * (2 * T * D);
   const uint16_t* vt = kt + 2 * T * D;
   for (int t = t0; t < end; t += stride) {
-    f4 sc[RT][2];
+    f4 sc[1][RT][2];
 #pragma unroll
-    for (int r = 0; r < RT; ++r) sc[r][0] = sc[r][1] = (f4){0.0f, 0.0f, 0.0f, 0.0f};
+    for (int r = 0; r < RT; ++r) sc[0][r][0] = sc[0][r][1] = (f4){0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) {
       const int ch = (i >> 1) * 64 + quad * 16 + (i & 1) * 8;
@@ -434,14 +440,16 @@ __device__ __forceinline__ void unfinished_block(const DenseAttnParams& p, State
         u4 q = {0, 0, 0, 0};
         if (lim[r] != 0x7fffffff) q = load_query(p, b, g, row0 + r * 16 + col, ch);
 #pragma unroll
-        for (int a = 0; a < 2; ++a) sc[r][a] = mfma_raw(k[a], q, sc[r][a], bf16);
+        for (int a = 0; a < 2; ++a) sc[0][r][a] = mfma_raw(k[a], q, sc[0][r][a], bf16);
       }
     }
-    float fk[RT][2];
+    float fk[1][RT][2];
 #pragma unroll
-    for (int r = 0; r < RT; ++r) fk[r][0] = fk[r][1] = p.scale_log2;
-    float pr[RT][8];
-    softmax_step<D, RT, SUMS>(s, sc, fk, lim, lim_lo, t, ctx, 0.0f, 0.0f, col, quad, sums, pr);
+    for (int r = 0; r < RT; ++r) fk[0][r][0] = fk[0][r][1] = p.scale_log2;
+    const float lsv[2] = {0.0f, 0.0f};
+    float d[2], pr[RT][8];
+    begin_steps<D, RT, 1>(s, sc, fk, lim, lim_lo, t, ctx, lsv, quad, d);
+    finish_step<D, RT, SUMS>(s, sc[0], fk[0], d, t, ctx, col, quad, sums, pr);
     u4 pa[RT], pb[RT];                              // fp16; or two bf16 parts
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
@@ -633,25 +641,26 @@ __global__ __launch_bounds__(256, 2) void dense_split_kernel(const DenseAttnPara
   // ---- finished blocks
   auto compute = [&](const Tile<D>& y, int i) {
     const int t = tw + i * kRound;
-    f4 sc[RT][2];
-    float fk[RT][2];
+    f4 sc[1][RT][2];
+    float fk[1][RT][2];
 #pragma unroll
     for (int a = 0; a < 2; ++a) {
 #pragma unroll
-      for (int r = 0; r < RT; ++r) sc[r][a] = (f4){0.0f, 0.0f, 0.0f, 0.0f};
+      for (int r = 0; r < RT; ++r) sc[0][r][a] = (f4){0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
       for (int n = 0; n < N; ++n)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const h8 k = code8<E4M3>(y.k[a][n][2 * h], y.k[a][n][2 * h + 1]);
 #pragma unroll
-          for (int r = 0; r < RT; ++r) sc[r][a] = mfma_f16(k, q[r][2 * n + h], sc[r][a]);
+          for (int r = 0; r < RT; ++r) sc[0][r][a] = mfma_f16(k, q[r][2 * n + h], sc[0][r][a]);
         }
 #pragma unroll
-      for (int r = 0; r < RT; ++r) fk[r][a] = y.sk[a] * qs[r];
+      for (int r = 0; r < RT; ++r) fk[0][r][a] = y.sk[a] * qs[r];
     }
-    float pr[RT][8];
-    softmax_step<D, RT, SUMS>(s, sc, fk, lim, lim_lo, t, e8, y.lsv[0], y.lsv[1], col, quad, sums, pr);
+    float d[2], pr[RT][8];
+    begin_steps<D, RT, 1>(s, sc, fk, lim, lim_lo, t, e8, y.lsv, quad, d);
+    finish_step<D, RT, SUMS>(s, sc[0], fk[0], d, t, e8, col, quad, sums, pr);
     h8 ph[RT];
     to_operand<RT>(pr, ph);
 #pragma unroll
@@ -899,26 +908,29 @@ __global__ __launch_bounds__(256, 2) void dense_chunk_kernel(const DenseAttnPara
         if (i + 2 < n) load(((i + 2) & 15) == 0 ? next : now, i + 2);
         const uint8_t* buf = lds[i & 1];
         const int t = t0 + i * kTile;
+        // both steps' scores first: the second's exponentials run beside the first's products
+        f4 sc[2][RT][2];
+        float fk[2][RT][2], d[4];
 #pragma unroll
-        for (int st = 0; st < 2; ++st) {
-          f4 sc[RT][2];
-          float fk[RT][2];
+        for (int st = 0; st < 2; ++st)
 #pragma unroll
           for (int a = 0; a < 2; ++a) {
 #pragma unroll
-            for (int r = 0; r < RT; ++r) sc[r][a] = (f4){0.0f, 0.0f, 0.0f, 0.0f};
+            for (int r = 0; r < RT; ++r) sc[st][r][a] = (f4){0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int k = 0; k < 2 * N; ++k) {
               const h8 kf = *reinterpret_cast<const h8*>(buf + ((st * 2 + a) * 2 * N + k) * kFrag + lane * 16);
 #pragma unroll
-              for (int r = 0; r < RT; ++r) sc[r][a] = mfma_f16(kf, q[r][k], sc[r][a]);
+              for (int r = 0; r < RT; ++r) sc[st][r][a] = mfma_f16(kf, q[r][k], sc[st][r][a]);
             }
 #pragma unroll
-            for (int r = 0; r < RT; ++r) fk[r][a] = sk[st * 2 + a] * qs[r];
+            for (int r = 0; r < RT; ++r) fk[st][r][a] = sk[st * 2 + a] * qs[r];
           }
+        begin_steps<D, RT, 2>(s, sc, fk, lim, lim_lo, t, e8, lsv, quad, d);
+#pragma unroll
+        for (int st = 0; st < 2; ++st) {
           float pr[RT][8];
-          softmax_step<D, RT, false>(s, sc, fk, lim, lim_lo, t + st * 32, e8, lsv[st * 2],
-                                     lsv[st * 2 + 1], col, quad, none, pr);
+          finish_step<D, RT, false>(s, sc[st], fk[st], d + 2 * st, t, e8, col, quad, none, pr);
           h8 ph[RT];
           to_operand<RT>(pr, ph);
 #pragma unroll
