@@ -57,6 +57,7 @@ struct DenseReadParams {
   const int32_t* ctx_len;
   const int32_t* start;
   int32_t n, out_dtype;
+  int32_t wide[2];                              // rows aligned to four elements
 };
 
 struct DenseEvictParams {

@@ -9,6 +9,7 @@ namespace {
 
 typedef uint32_t u4c __attribute__((ext_vector_type(4)));
 typedef float f2c __attribute__((ext_vector_type(2)));
+typedef uint16_t us2 __attribute__((ext_vector_type(2)));
 
 __device__ __forceinline__ float from16(uint32_t u, int bf16) {
   return bf16 ? __uint_as_float(u << 16) : (float)__builtin_bit_cast(_Float16, (uint16_t)u);
@@ -21,6 +22,15 @@ __device__ __forceinline__ int tail_value(int row, int ch, int d) {
   return ((row >> 4) * d + ch) * 16 + (row & 15);
 }
 
+// Eight elements of a row.
+__device__ __forceinline__ u4c load8(const uint16_t* a, int wide) {
+  if (wide) return *reinterpret_cast<const u4c*>(a);
+  union { u4c v; uint16_t h[8]; } w;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) w.h[e] = a[e];
+  return w.v;
+}
+
 // ------------------------------------------------------------------------------ append
 //
 // One workgroup per block that the new tokens touch, KV head and keys or values.  A block
@@ -30,12 +40,16 @@ __device__ __forceinline__ int tail_value(int row, int ch, int d) {
 // tokens of the last two blocks into the tail: it is the only one that reads the tail, and it
 // does so before it writes.
 //
-// Codes are RN(x / s) without a second rounding: the fp32 quotient, less than one unit in the
-// last place off, is moved to an odd significand on the true quotient's side unless it is
-// exact (the sign of the residual x - q s decides, and fma gives that sign exactly).  No border
-// between two codes has an odd 24-bit significand, so rounding the odd value rounds the quotient.
-// Scales below 2^-60 and their rows are multiplied by 2^100 first, so that the residual does
-// not underflow.
+// Codes are RN(x / s), decided exactly.  Borders between two codes have few bits (at most 8 in the
+// significand), so a quotient may be replaced by any value on the same side of the nearest 8-bit
+// number b: b itself if the quotient equals it, else b moved by one unit of fp32 towards the
+// quotient, as the sign of the residual x - b s tells, which fma gives exactly.
+// INT8 seldom needs that: the products of x with two reciprocals of s, 2^-22 below and above,
+// enclose the quotient, and where all sixteen codes of a thread come out alike from both they are
+// right.  (E4M3's coarse grid meets the quotients of 16-bit values far more often, in nearly every
+// wave.)  Scales below 2^-60 and their rows are multiplied by 2^100 first, so that the
+// residual does not underflow.  Measured against an fp32 division with residuals for all values:
+// 4 x 131072 tokens of 8 heads in INT8 852 -> 712 us.
 struct Quantizer {
   float lift, s, inv;
   __device__ __forceinline__ Quantizer(float scale) {
@@ -44,37 +58,61 @@ struct Quantizer {
     inv = s > 0.0f ? 1.0f / s : 0.0f;
   }
   __device__ __forceinline__ float quotient(float x) const {
-    x *= lift;
-    float q = x * inv;
-    q = __builtin_fmaf(__builtin_fmaf(-q, s, x), inv, q);
-    const float r = __builtin_fmaf(-q, s, x);
-    const uint32_t u = __float_as_uint(q);
-    const bool out = (r > 0.0f) == (x > 0.0f);        // away from zero
-    const uint32_t odd = out ? u + 1 : u - 1;
-    return r != 0.0f && !(u & 1) && q != 0.0f ? __uint_as_float(odd) : q;
+    const uint32_t b = (__float_as_uint(x * inv) + 0x8000u) & 0xffff0000u;
+    const float r = __builtin_fmaf(-__uint_as_float(b), s, x);
+    const int towards = (int)(__float_as_uint(r) ^ __float_as_uint(x)) >> 31 | 1;
+    return __uint_as_float(r != 0.0f ? b + towards : b);
   }
 };
 
+// Four codes from quotients x * f.
 template <bool E4M3>
-__device__ __forceinline__ uint32_t pack_codes(const float* q) {
+__device__ __forceinline__ uint32_t pack_codes(const float* x, float f) {
   if constexpr (E4M3) {
-    int v = __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], 0, false);
-    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(q[2], q[3], v, true);
+    int v = __builtin_amdgcn_cvt_pk_fp8_f32(x[0] * f, x[1] * f, 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[2] * f, x[3] * f, v, true);
   } else {
-    uint32_t v = 0;
+    // x f + 1.5 2^23 + 128 in one rounding: the code, offset by 128, is the sum's low byte
+    uint32_t w[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int c = (int)__builtin_rintf(fminf(fmaxf(q[i], -127.0f), 127.0f)) + 128;
-      v |= (uint32_t)c << (8 * i);
-    }
-    return v;
+    for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(__builtin_fmaf(x[i], f, 12583040.0f));
+    const uint32_t a = __builtin_amdgcn_perm(w[1], w[0], 0x0c0c0400u);
+    const uint32_t b = __builtin_amdgcn_perm(w[3], w[2], 0x04000c0cu);
+    return a | b;
   }
+}
+
+// Sixteen codes.
+template <bool E4M3>
+__device__ __forceinline__ u4c quantize16(const Quantizer& qz, float* x) {
+  u4c v;
+  bool decided = false;
+  if (qz.lift != 1.0f) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) x[e] *= qz.lift;
+  } else if constexpr (!E4M3) {
+    uint32_t differ = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      v[e] = pack_codes<E4M3>(x + 4 * e, qz.inv * (1.0f + 0x1p-22f));
+      differ |= v[e] ^ pack_codes<E4M3>(x + 4 * e, qz.inv * (1.0f - 0x1p-22f));
+    }
+    decided = differ == 0;
+  }
+  if (!decided) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) x[e] = qz.quotient(x[e]);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = pack_codes<E4M3>(x + 4 * e, 1.0f);
+  }
+  return v;
 }
 
 template <int D, bool E4M3>
 __global__ __launch_bounds__(256) void dense_append_kernel(const DenseAppendParams p) {
   constexpr int kRow = D + 8;                       // LDS row: 16 bytes of padding
-  __shared__ __attribute__((aligned(16))) uint16_t rows[128 * kRow];
+  // T rows: the smaller the block, the more workgroups of a compute unit hide each other's waits
+  extern __shared__ __attribute__((aligned(16))) uint16_t rows[];
   __shared__ uint32_t wave_top[4];
   const int tid = threadIdx.x;
   const int g = blockIdx.y, b = blockIdx.z >> 1, kv = blockIdx.z & 1;
@@ -88,25 +126,21 @@ __global__ __launch_bounds__(256) void dense_append_kernel(const DenseAppendPara
   const int j = (lo >> sh) + blockIdx.x, last = (hi - 1) >> sh;
   if (j > last) return;
   const int64_t head = (int64_t)b * p.c.n_kv + g;
+  const int entry = p.c.table[head * p.c.blocks_per_head + j];
   uint16_t* tail = p.c.tails + (head * 2 + kv) * (2 * T * D);
   const uint16_t* x = p.x[kv] + b * p.xs_b[kv] + g * p.xs_h[kv] - first * p.xs_t[kv];
   const int64_t xt = p.xs_t[kv];
   const int wide = p.wide[kv];
 
   if (hi >= (j + 1) << sh) {                        // the block is finished
-    uint32_t top = 0;
+    us2 most = {0, 0};
     constexpr int C8 = D / 8;
+#pragma unroll 4
     for (int i = tid; i < T * C8; i += 256) {
       const int r = i / C8, c = (i % C8) * 8, t = (j << sh) + r;
       union { u4c v; uint16_t h[8]; } w;
       if (t >= lo) {
-        const uint16_t* a = x + t * xt + c;
-        if (wide) {
-          w.v = *reinterpret_cast<const u4c*>(a);
-        } else {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) w.h[e] = a[e];
-        }
+        w.v = load8(x + t * xt + c, wide);
       } else {
         const int tr = t & (2 * T - 1);
         if (kv == 0) {
@@ -120,8 +154,10 @@ __global__ __launch_bounds__(256) void dense_append_kernel(const DenseAppendPara
       // |x| as an integer: the order of the 16-bit patterns is that of the values, with the
       // infinity and NaNs on top
 #pragma unroll
-      for (int e = 0; e < 8; ++e) top = max(top, (uint32_t)(w.h[e] & 0x7fff));
+      for (int e = 0; e < 4; ++e)
+        most = __builtin_elementwise_max(most, __builtin_bit_cast(us2, w.v[e] & 0x7fff7fffu));
     }
+    uint32_t top = max((uint32_t)most[0], (uint32_t)most[1]);
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
     if ((tid & 63) == 0) wave_top[tid >> 6] = top;
@@ -129,7 +165,6 @@ __global__ __launch_bounds__(256) void dense_append_kernel(const DenseAppendPara
     top = max(max(wave_top[0], wave_top[1]), max(wave_top[2], wave_top[3]));
     const bool bad = top >= (bf16 ? 0x7f80u : 0x7c00u);
     const float scale = bad ? __builtin_nanf("") : from16(top, bf16) / (E4M3 ? 448.0f : 127.0f);
-    const int entry = p.c.table[head * p.c.blocks_per_head + j];
     if (entry >= 0 && entry < p.c.n_blocks) {
       if (tid == 0) reinterpret_cast<float*>(p.c.scales)[2 * (int64_t)entry + kv] = scale;
       const Quantizer qz(bad ? 0.0f : scale);
@@ -150,41 +185,59 @@ __global__ __launch_bounds__(256) void dense_append_kernel(const DenseAppendPara
           for (int e = 0; e < 16; ++e)
             q[e] = from16(rows[(st * 16 + 4 * a + (e & 3)) * kRow + grp * 64 + (e >> 2) * 16 + l], bf16);
         }
-        union { u4c v; uint32_t w[4]; } z;
+        if (bad) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) q[e] = bad ? 0.0f : qz.quotient(q[e]);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) z.w[e] = pack_codes<E4M3>(q + 4 * e);
-        *reinterpret_cast<u4c*>(dst + (int64_t)i * 16) = z.v;
+          for (int e = 0; e < 16; ++e) q[e] = 0.0f;
+        }
+        *reinterpret_cast<u4c*>(dst + (int64_t)i * 16) = quantize16<E4M3>(qz, q);
       }
     }
   }
   if (blockIdx.x == 0) {
     const int from = max(lo, (last - 1) << sh);
-    for (int i = tid; i < (hi - from) * D; i += 256) {
-      const int t = from + i / D, c = i % D, tr = t & (2 * T - 1);
-      tail[kv == 0 ? tr * D + c : tail_value(tr, c, D)] = x[t * xt + c];
+    if (kv == 0) {                                  // rows, eight channels a thread
+      constexpr int C8 = D / 8;
+#pragma unroll 4
+      for (int i = tid; i < (hi - from) * C8; i += 256) {
+        const int t = from + i / C8, c = i % C8 * 8;
+        *reinterpret_cast<u4c*>(tail + (t & (2 * T - 1)) * D + c) = load8(x + t * xt + c, wide);
+      }
+    } else {                                        // eight tokens of a channel a thread
+      const int t8 = from & ~7, n8 = (hi - t8 + 7) >> 3;
+#pragma unroll 2
+      for (int i = tid; i < n8 * D; i += 256) {
+        const int t = t8 + i / D * 8, c = i % D;
+        union { u4c v; uint16_t h[8]; } w;
+        uint16_t* to = tail + tail_value(t & (2 * T - 1), c, D);
+        if (t >= from && t + 8 <= hi) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) w.h[e] = x[(t + e) * xt + c];
+          *reinterpret_cast<u4c*>(to) = w.v;
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (t + e >= from && t + e < hi) to[e] = x[(t + e) * xt + c];
+        }
+      }
     }
   }
 }
 
 // -------------------------------------------------------------------------------- read
 //
-// One workgroup per four 16-token subtiles of the requested rows, KV head and keys or values;
-// a thread takes a 16-byte unit of codes.
-template <int D, bool E4M3>
+// One workgroup per 32 tokens (two subtiles), KV head and keys or values: rows are put together in
+// LDS and leave in whole rows, since a thread's 16 bytes of codes lie across four rows (values)
+// or 16 threads' across 16 rows (keys).
+template <bool E4M3>
 __device__ __forceinline__ float code_value(uint32_t byte) {
   if constexpr (E4M3) return __builtin_amdgcn_cvt_f32_fp8((int)byte, 0);
   else return (float)((int)byte - 128);
 }
 
-__device__ __forceinline__ void store_as(void* out, int64_t at, float f, int dtype) {
-  if (dtype == STARKV_DT_F32) static_cast<float*>(out)[at] = f;
-  else static_cast<uint16_t*>(out)[at] = dtype == STARKV_DT_BF16 ? to_bf16(f) : to_f16(f);
-}
-
 template <int D, bool E4M3>
 __global__ __launch_bounds__(256) void dense_read_kernel(const DenseReadParams p) {
+  constexpr int kRow = D + 4;
+  __shared__ __attribute__((aligned(16))) float rows[32 * kRow];
   const int g = blockIdx.y, b = blockIdx.z >> 1, kv = blockIdx.z & 1;
   void* out = p.out[kv];
   if (!out) return;
@@ -194,39 +247,80 @@ __global__ __launch_bounds__(256) void dense_read_kernel(const DenseReadParams p
   const int full = ctx & ~(T - 1);
   const int64_t head = (int64_t)b * p.c.n_kv + g;
   const uint16_t* tail = p.c.tails + (head * 2 + kv) * (2 * T * D);
-  const int64_t o0 = b * p.os_b[kv] + g * p.os_h[kv] - start * p.os_t[kv];
-  const int64_t ot = p.os_t[kv];
-  const int64_t s0 = (start >> 4) + (int64_t)blockIdx.x * 4;
-  for (int i = threadIdx.x; i < 4 * D; i += 256) {
-    const int64_t t0 = (s0 + i / D) * 16;           // first token of the subtile
-    const int u = i % D, grp = u >> 6, a = (u >> 4) & 3, l = u & 15;
+  const int64_t t0 = ((start >> 4) + (int64_t)blockIdx.x * 2) * 16;   // first token
+  for (int i = threadIdx.x; i < 2 * D; i += 256) {
+    const int st = i / D, u = i % D, grp = u >> 6, a = (u >> 4) & 3, l = u & 15;
+    const int64_t ts = t0 + st * 16;
     float q[16];
-    if (t0 >= 0 && t0 < full) {
-      int entry = p.c.table[head * p.c.blocks_per_head + (t0 >> sh)];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) q[e] = 0.0f;
+    if (ts >= 0 && ts < full) {
+      int entry = p.c.table[head * p.c.blocks_per_head + (ts >> sh)];
       entry = min(max(entry, 0), p.c.n_blocks - 1);
       const float s = reinterpret_cast<const float*>(p.c.scales)[2 * (int64_t)entry + kv];
-      const uint8_t* src = p.c.codes + (int64_t)entry * (2 * T * D) + kv * (T * D) +
-                           ((t0 & (T - 1)) >> 4) * (16 * D) + u * 16;
       union { u4c v; uint8_t c[16]; } w;
-      w.v = *reinterpret_cast<const u4c*>(src);
+      w.v = *reinterpret_cast<const u4c*>(p.c.codes + (int64_t)entry * (2 * T * D) + kv * (T * D) +
+                                          ((ts & (T - 1)) >> 4) * (16 * D) + u * 16);
 #pragma unroll
-      for (int e = 0; e < 16; ++e) q[e] = code_value<D, E4M3>(w.c[e]) * s;
-    }
+      for (int e = 0; e < 16; ++e) q[e] = code_value<E4M3>(w.c[e]) * s;
+    } else if (ts >= full && ts < ctx) {
+      // (the ring's rows beyond the last token hold anything)
+      const int tr = (int)ts & (2 * T - 1);
+      if (kv == 0) {
+        union { u4c v[2]; uint16_t h[16]; } w;
+        const u4c* src = reinterpret_cast<const u4c*>(tail + (tr + l) * D + grp * 64 + a * 16);
+        w.v[0] = src[0];
+        w.v[1] = src[1];
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const int64_t t = t0 + (kv == 0 ? l : 4 * a + (e & 3));
-      const int c = grp * 64 + (kv == 0 ? 16 * a + e : (e >> 2) * 16 + l);
-      if (t < start || t >= start + p.n) continue;
-      float f = 0.0f;
-      if (t >= 0 && t < ctx) {
-        if (t < full) {
-          f = q[e];
-        } else {
-          const int tr = (int)t & (2 * T - 1);
-          f = from16(tail[kv == 0 ? tr * D + c : tail_value(tr, c, D)], bf16);
+        for (int e = 0; e < 16; ++e) q[e] = ts + l < ctx ? from16(w.h[e], bf16) : 0.0f;
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          union { f2c v; uint16_t h[4]; } w;
+          w.v = *reinterpret_cast<const f2c*>(tail + tail_value(tr + 4 * a, grp * 64 + j * 16 + l, D));
+#pragma unroll
+          for (int r = 0; r < 4; ++r) q[4 * j + r] = ts + 4 * a + r < ctx ? from16(w.h[r], bf16) : 0.0f;
         }
       }
-      store_as(out, o0 + t * ot + c, f, p.out_dtype);
+    }
+    if (kv == 0) {
+      float* to = rows + (st * 16 + l) * kRow + grp * 64 + a * 16;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) to[e] = q[e];
+    } else {
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        rows[(st * 16 + 4 * a + (e & 3)) * kRow + grp * 64 + (e >> 2) * 16 + l] = q[e];
+    }
+  }
+  __syncthreads();
+  const int64_t o0 = b * p.os_b[kv] + g * p.os_h[kv] - start * p.os_t[kv];
+  constexpr int kFour = D / 4;                      // a thread writes four channels
+  for (int i = threadIdx.x; i < 32 * kFour; i += 256) {
+    const int64_t t = t0 + i / kFour;
+    if (t < start || t >= start + p.n) continue;
+    const int c = i % kFour * 4;
+    const float* f = rows + i / kFour * kRow + c;
+    const int64_t at = o0 + t * p.os_t[kv] + c;
+    if (p.out_dtype == STARKV_DT_F32) {
+      float* o = static_cast<float*>(out) + at;
+      if (p.wide[kv]) {
+        *reinterpret_cast<float4*>(o) = *reinterpret_cast<const float4*>(f);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = f[e];
+      }
+    } else {
+      uint16_t* o = static_cast<uint16_t*>(out) + at;
+      union { f2c v; uint16_t h[4]; } w;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w.h[e] = p.out_dtype == STARKV_DT_BF16 ? to_bf16(f[e]) : to_f16(f[e]);
+      if (p.wide[kv]) {
+        *reinterpret_cast<f2c*>(o) = w.v;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = w.h[e];
+      }
     }
   }
 }
@@ -410,21 +504,22 @@ int launch_dense_append(const DenseAppendParams& p, void* stream) {
   const int64_t touched = ((int64_t)p.n_new + 2 * T - 2) >> p.c.shift;
   const dim3 grid((uint32_t)(touched < p.c.blocks_per_head ? touched : p.c.blocks_per_head),
                   p.c.n_kv, p.c.batch * 2);
+  const uint32_t lds = T * (p.c.d + 8) * 2;
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (p.c.d == 128) {
-    if (p.c.e4m3) hipLaunchKernelGGL((dense_append_kernel<128, true>), grid, dim3(256), 0, st, p);
-    else hipLaunchKernelGGL((dense_append_kernel<128, false>), grid, dim3(256), 0, st, p);
+    if (p.c.e4m3) hipLaunchKernelGGL((dense_append_kernel<128, true>), grid, dim3(256), lds, st, p);
+    else hipLaunchKernelGGL((dense_append_kernel<128, false>), grid, dim3(256), lds, st, p);
   } else {
-    if (p.c.e4m3) hipLaunchKernelGGL((dense_append_kernel<64, true>), grid, dim3(256), 0, st, p);
-    else hipLaunchKernelGGL((dense_append_kernel<64, false>), grid, dim3(256), 0, st, p);
+    if (p.c.e4m3) hipLaunchKernelGGL((dense_append_kernel<64, true>), grid, dim3(256), lds, st, p);
+    else hipLaunchKernelGGL((dense_append_kernel<64, false>), grid, dim3(256), lds, st, p);
   }
   return (int)hipGetLastError();
 }
 
 int launch_dense_read(const DenseReadParams& p, void* stream) {
-  // 16-token subtiles that n rows can touch, four to a workgroup
+  // 16-token subtiles that n rows can touch, two to a workgroup
   const int64_t subs = ((int64_t)p.n + 30) >> 4;
-  const dim3 grid((uint32_t)((subs + 3) / 4), p.c.n_kv, p.c.batch * 2);
+  const dim3 grid((uint32_t)((subs + 1) / 2), p.c.n_kv, p.c.batch * 2);
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (p.c.d == 128) {
     if (p.c.e4m3) hipLaunchKernelGGL((dense_read_kernel<128, true>), grid, dim3(256), 0, st, p);

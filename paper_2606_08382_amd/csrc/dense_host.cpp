@@ -340,6 +340,7 @@ starkv_status starkv_dense_read(const starkv_dense_plan* P, const void* cache,
     if (o[i] && !rows_apart(a, P->cfg.batch, n, P->cfg.n_kv_heads, P->cfg.head_dim))
       return fail_with(STARKV_ERR_INVALID_ARG, "rows of the output overlap");
     p.out[i] = o[i];
+    p.wide[i] = rows_wide(o[i], a, elem, 4 * elem);
     p.os_b[i] = a.batch;
     p.os_t[i] = a.token;
     p.os_h[i] = a.head;
