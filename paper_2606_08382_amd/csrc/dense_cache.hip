@@ -33,8 +33,8 @@ __device__ __forceinline__ u4c load8(const uint16_t* a, int wide) {
 
 // ------------------------------------------------------------------------------ append
 //
-// One workgroup per block that the new tokens touch, KV head and keys or values.  A block
-// that they finish is gathered into LDS (its earlier tokens from the 16-bit tail), its
+// One workgroup per 64 tokens (or a block of 128) of the blocks that the new tokens touch, KV head
+// and keys or values.  A block that they finish is gathered into LDS (its earlier tokens from the 16-bit tail), its
 // absolute maximum taken on the bit patterns, and its codes written in the order that the
 // attention's matrix operands take (see the header).  The first workgroup also moves the new
 // tokens of the last two blocks into the tail: it is the only one that reads the tail, and it
@@ -108,36 +108,43 @@ __device__ __forceinline__ u4c quantize16(const Quantizer& qz, float* x) {
   return v;
 }
 
-template <int D, bool E4M3>
+template <int D, bool E4M3, int SH>
 __global__ __launch_bounds__(256) void dense_append_kernel(const DenseAppendParams p) {
-  constexpr int kRow = D + 8;                       // LDS row: 16 bytes of padding
-  // T rows: the smaller the block, the more workgroups of a compute unit hide each other's waits
-  extern __shared__ __attribute__((aligned(16))) uint16_t rows[];
-  __shared__ uint32_t wave_top[4];
+  constexpr int T = 1 << SH, W = T < 64 ? 64 : T;   // tokens of a block, of a workgroup
+  constexpr int kBlocks = W / T, kRow = D + 8, C8 = D / 8;   // (LDS row: 16 bytes of padding)
+  __shared__ __attribute__((aligned(16))) uint16_t rows[W * kRow];
+  __shared__ uint32_t wave_top[kBlocks][4];
   const int tid = threadIdx.x;
-  const int g = blockIdx.y, b = blockIdx.z >> 1, kv = blockIdx.z & 1;
-  const int sh = p.c.shift, T = 1 << sh, bf16 = p.c.bf16;
+  const int g = blockIdx.y, b = blockIdx.z >> 1, kv = blockIdx.z & 1, bf16 = p.c.bf16;
   const int64_t first = p.pos[b];
   const int m = p.n_new_dev ? min(max(p.n_new_dev[b], 0), p.n_new) : p.n_new;
   const int64_t hi64 = first + m;
   const int lo = (int)min(max(first, (int64_t)0), (int64_t)p.c.capacity);
   const int hi = (int)min(max(hi64, (int64_t)0), (int64_t)p.c.capacity);
   if (lo >= hi) return;
-  const int j = (lo >> sh) + blockIdx.x, last = (hi - 1) >> sh;
-  if (j > last) return;
+  const int j0 = (lo >> SH) + blockIdx.x * kBlocks, last = (hi - 1) >> SH;
+  if (j0 > last) return;
+  const int n = min((hi >> SH) - j0, kBlocks);      // finished blocks of the workgroup
   const int64_t head = (int64_t)b * p.c.n_kv + g;
-  const int entry = p.c.table[head * p.c.blocks_per_head + j];
+  const int32_t* table = p.c.table + head * p.c.blocks_per_head;
   uint16_t* tail = p.c.tails + (head * 2 + kv) * (2 * T * D);
   const uint16_t* x = p.x[kv] + b * p.xs_b[kv] + g * p.xs_h[kv] - first * p.xs_t[kv];
   const int64_t xt = p.xs_t[kv];
   const int wide = p.wide[kv];
 
-  if (hi >= (j + 1) << sh) {                        // the block is finished
-    us2 most = {0, 0};
-    constexpr int C8 = D / 8;
-#pragma unroll 4
-    for (int i = tid; i < T * C8; i += 256) {
-      const int r = i / C8, c = (i % C8) * 8, t = (j << sh) + r;
+  if (n > 0) {
+    int entry[kBlocks];
+#pragma unroll
+    for (int k = 0; k < kBlocks; ++k) entry[k] = k < n ? table[j0 + k] : -1;
+    // a block's rows take whole waves of every pass, so its maximum is one over waves
+    constexpr int kPass = 256 / C8;                 // rows of a pass
+    us2 most[kBlocks];
+#pragma unroll
+    for (int k = 0; k < kBlocks; ++k) most[k] = (us2){0, 0};
+#pragma unroll
+    for (int r0 = 0; r0 < W; r0 += kPass) {
+      const int r = r0 + tid / C8, c = (tid % C8) * 8, t = j0 * T + r;
+      if (r >= n * T) continue;
       union { u4c v; uint16_t h[8]; } w;
       if (t >= lo) {
         w.v = load8(x + t * xt + c, wide);
@@ -154,28 +161,39 @@ __global__ __launch_bounds__(256) void dense_append_kernel(const DenseAppendPara
       // |x| as an integer: the order of the 16-bit patterns is that of the values, with the
       // infinity and NaNs on top
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        most = __builtin_elementwise_max(most, __builtin_bit_cast(us2, w.v[e] & 0x7fff7fffu));
-    }
-    uint32_t top = max((uint32_t)most[0], (uint32_t)most[1]);
+      for (int k = 0; k < kBlocks; ++k)
+        if (r >> SH == k)
 #pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
-    if ((tid & 63) == 0) wave_top[tid >> 6] = top;
+          for (int e = 0; e < 4; ++e)
+            most[k] = __builtin_elementwise_max(most[k], __builtin_bit_cast(us2, w.v[e] & 0x7fff7fffu));
+    }
+#pragma unroll
+    for (int k = 0; k < kBlocks; ++k) {
+      uint32_t top = max((uint32_t)most[k][0], (uint32_t)most[k][1]);
+#pragma unroll
+      for (int o = 32; o >= 1; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
+      if ((tid & 63) == 0) wave_top[k][tid >> 6] = top;
+    }
     __syncthreads();
-    top = max(max(wave_top[0], wave_top[1]), max(wave_top[2], wave_top[3]));
-    const bool bad = top >= (bf16 ? 0x7f80u : 0x7c00u);
-    const float scale = bad ? __builtin_nanf("") : from16(top, bf16) / (E4M3 ? 448.0f : 127.0f);
-    if (entry >= 0 && entry < p.c.n_blocks) {
-      if (tid == 0) reinterpret_cast<float*>(p.c.scales)[2 * (int64_t)entry + kv] = scale;
+#pragma unroll
+    for (int k = 0; k < kBlocks; ++k) {
+      if (entry[k] < 0 || entry[k] >= p.c.n_blocks) continue;
+      const uint32_t top = max(max(wave_top[k][0], wave_top[k][1]), max(wave_top[k][2], wave_top[k][3]));
+      const bool bad = top >= (bf16 ? 0x7f80u : 0x7c00u);
+      const float scale = bad ? __builtin_nanf("") : from16(top, bf16) / (E4M3 ? 448.0f : 127.0f);
+      if (tid == 0) reinterpret_cast<float*>(p.c.scales)[2 * (int64_t)entry[k] + kv] = scale;
       const Quantizer qz(bad ? 0.0f : scale);
-      uint8_t* dst = p.c.codes + (int64_t)entry * (2 * T * D) + kv * (T * D);
-      for (int i = tid; i < T * D / 16; i += 256) {
+      uint8_t* dst = p.c.codes + (int64_t)entry[k] * (2 * T * D) + kv * (T * D);
+#pragma unroll
+      for (int i0 = 0; i0 < T * D / 16; i0 += 256) {
+        const int i = i0 + tid;
+        if (T * D / 16 < 256 && i >= T * D / 16) continue;
         const int st = i / D, u = i % D;            // subtile, its 16-byte unit
         const int grp = u >> 6, a = (u >> 4) & 3, l = u & 15;
         float q[16];
         if (kv == 0) {                              // token l, channels grp*64 + 16a ..
           union { u4c v[2]; uint16_t h[16]; } w;
-          const uint16_t* s = rows + (st * 16 + l) * kRow + grp * 64 + a * 16;
+          const uint16_t* s = rows + (k * T + st * 16 + l) * kRow + grp * 64 + a * 16;
           w.v[0] = *reinterpret_cast<const u4c*>(s);
           w.v[1] = *reinterpret_cast<const u4c*>(s + 8);
 #pragma unroll
@@ -183,7 +201,7 @@ __global__ __launch_bounds__(256) void dense_append_kernel(const DenseAppendPara
         } else {                                    // tokens 4a .., channels grp*64 + 16 jt + l
 #pragma unroll
           for (int e = 0; e < 16; ++e)
-            q[e] = from16(rows[(st * 16 + 4 * a + (e & 3)) * kRow + grp * 64 + (e >> 2) * 16 + l], bf16);
+            q[e] = from16(rows[(k * T + st * 16 + 4 * a + (e & 3)) * kRow + grp * 64 + (e >> 2) * 16 + l], bf16);
         }
         if (bad) {
 #pragma unroll
@@ -194,9 +212,8 @@ __global__ __launch_bounds__(256) void dense_append_kernel(const DenseAppendPara
     }
   }
   if (blockIdx.x == 0) {
-    const int from = max(lo, (last - 1) << sh);
+    const int from = max(lo, (last - 1) << SH);
     if (kv == 0) {                                  // rows, eight channels a thread
-      constexpr int C8 = D / 8;
 #pragma unroll 4
       for (int i = tid; i < (hi - from) * C8; i += 256) {
         const int t = from + i / C8, c = i % C8 * 8;
@@ -499,19 +516,30 @@ __global__ void dense_evict_ctx_kernel(const DenseEvictParams p) {
 
 }  // namespace
 
+namespace {
+template <int D, bool E4M3>
+void launch_append(const DenseAppendParams& p, dim3 grid, hipStream_t st) {
+#define SK_APPEND(SH) hipLaunchKernelGGL((dense_append_kernel<D, E4M3, SH>), grid, dim3(256), 0, st, p)
+  if (p.c.shift == 4) SK_APPEND(4);
+  else if (p.c.shift == 5) SK_APPEND(5);
+  else if (p.c.shift == 6) SK_APPEND(6);
+  else SK_APPEND(7);
+#undef SK_APPEND
+}
+}  // namespace
+
 int launch_dense_append(const DenseAppendParams& p, void* stream) {
-  const int T = 1 << p.c.shift;
+  const int T = 1 << p.c.shift, per = T < 64 ? 64 / T : 1;   // blocks of a workgroup
   const int64_t touched = ((int64_t)p.n_new + 2 * T - 2) >> p.c.shift;
-  const dim3 grid((uint32_t)(touched < p.c.blocks_per_head ? touched : p.c.blocks_per_head),
-                  p.c.n_kv, p.c.batch * 2);
-  const uint32_t lds = T * (p.c.d + 8) * 2;
+  const int64_t blocks = touched < p.c.blocks_per_head ? touched : p.c.blocks_per_head;
+  const dim3 grid((uint32_t)((blocks + per - 1) / per), p.c.n_kv, p.c.batch * 2);
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (p.c.d == 128) {
-    if (p.c.e4m3) hipLaunchKernelGGL((dense_append_kernel<128, true>), grid, dim3(256), lds, st, p);
-    else hipLaunchKernelGGL((dense_append_kernel<128, false>), grid, dim3(256), lds, st, p);
+    if (p.c.e4m3) launch_append<128, true>(p, grid, st);
+    else launch_append<128, false>(p, grid, st);
   } else {
-    if (p.c.e4m3) hipLaunchKernelGGL((dense_append_kernel<64, true>), grid, dim3(256), lds, st, p);
-    else hipLaunchKernelGGL((dense_append_kernel<64, false>), grid, dim3(256), lds, st, p);
+    if (p.c.e4m3) launch_append<64, true>(p, grid, st);
+    else launch_append<64, false>(p, grid, st);
   }
   return (int)hipGetLastError();
 }
