@@ -25,6 +25,7 @@ struct RopeParams {
   int32_t units;                                // work units of a head: rotated, then copied
   int32_t rot_units;
   int32_t heads_per_thread, head_groups;
+  int32_t streaming;                            // more bytes than the caches hold
   float gain, sine;                             // factor on cos; on sin (its sign: inverse)
   double turns[kMaxRotaryPairs];                // f_j / 2 pi
 };

@@ -531,6 +531,15 @@ __device__ __forceinline__ void unfinished_block(const DenseAttnParams& p, State
   }
 }
 
+// Sixteen bytes of codes; past the caches where one wave alone reads them (5.8 TB/s with plain loads,
+// 6.7 with these).
+template <int READERS>
+__device__ __forceinline__ u4 load_codes(const uint8_t* a) {
+  const u4* v = reinterpret_cast<const u4*>(a);
+  if constexpr (READERS == 1) return __builtin_nontemporal_load(v);
+  else return *v;
+}
+
 // Up to 64 query rows of a KV head.  A workgroup's waves take 32-token steps in turn; with RG = 2
 // two row groups of 16 RT rows share the steps (a wave's state of 64 rows would leave one wave
 // per SIMD; the codes' second reader finds them in cache).
@@ -606,13 +615,12 @@ __global__ __launch_bounds__(256, 2) void dense_split_kernel(const DenseAttnPara
       x.lsv[a] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(en.lsv), l));
       const uint8_t* kb = p.c.codes + (uint64_t)sub * (16 * D) + lane * 16;
       const uint8_t* vb = p.c.codes + (uint64_t)(sub + v_sub) * (16 * D) + lane * 16;
-      // (streaming: a code is read once a step; 5.8 TB/s with plain loads, 6.7 with these)
 #pragma unroll
       for (int n = 0; n < N; ++n)
-        x.k[a][n] = __builtin_nontemporal_load(reinterpret_cast<const u4*>(kb + n * 1024));
+        x.k[a][n] = load_codes<RG>(kb + n * 1024);
 #pragma unroll
       for (int n = 0; n < N; ++n)
-        x.v[a][n] = __builtin_nontemporal_load(reinterpret_cast<const u4*>(vb + n * 1024));
+        x.v[a][n] = load_codes<RG>(vb + n * 1024);
     }
   };
   // A step's codes are loaded NB - 1 steps ahead, past the last one the last again; the entries of

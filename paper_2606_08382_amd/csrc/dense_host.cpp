@@ -177,12 +177,14 @@ starkv_status starkv_rope(const starkv_rope_plan* P, const void* x, const starkv
                     (p.interleaved ? R : R / 2) % E == 0;
   p.rot_units = wide ? (p.interleaved ? R : R / 2) / E : R / 2;
   p.units = p.rot_units + (wide ? (D - R) / E : D - R);
-  // Heads share a token's angles: a thread walks over as many as leave 2^17 threads (two waves
-  // per SIMD), at most eight.
-  int64_t per = p.tokens * p.units * n_heads >> 17;
-  per = std::min<int64_t>(std::max<int64_t>(per, 1), 8);
+  // Heads share a token's angles: a thread takes two, where that leaves 2^17 threads (two waves per
+  // SIMD).  More heads a thread leave too few rows in flight (16384 tokens of 40 heads: 60 us with
+  // two, 62 with three, 65 with four, 68 with eight, 82 with one).
+  const int64_t per = p.tokens * p.units * n_heads >= (int64_t)1 << 18 ? 2 : 1;
   p.heads_per_thread = (int32_t)per;
   p.head_groups = (n_heads + p.heads_per_thread - 1) / p.heads_per_thread;
+  // (half of the 256 MB of last-level cache)
+  p.streaming = p.tokens * n_heads * D * elem * 2 > (int64_t)128 << 20;
   const double threads = (double)p.tokens * p.head_groups * p.units;
   if (threads > 256.0 * 0x7fffffff)
     return fail_with(STARKV_ERR_UNSUPPORTED, "%lld tokens of %d heads in one call", (long long)p.tokens, n_heads);

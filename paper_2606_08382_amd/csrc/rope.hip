@@ -4,7 +4,8 @@
 // first R channels, a = position * f_j; the rest is copied.  Bound by its bytes, one read and
 // one write of every element, as long as the angles cost little: an angle belongs to (token,
 // pair) and serves every head, so a thread takes one unit of pairs (16-byte accesses) of a
-// token, computes its angles once and walks over several heads.
+// token and computes its angles once for two heads.  16384 tokens of 40 heads of 128 in bf16: 60 us,
+// 5.6 TB/s.
 //
 // An angle is position * f / 2 pi in turns, in fp64, minus its nearest integer (exact), and only
 // then fp32: at position 2^31 the turn's fraction is still known to 2^-22.  sincospif takes it
@@ -57,9 +58,24 @@ __device__ __forceinline__ void angle(const RopeParams& p, int pos, int j, float
   *s *= p.sine;
 }
 
+// Sixteen bytes of a row.  Calls larger than the caches pass them by (336 MB: 60 us against 68);
+// the rows of smaller ones stay for what reads them next.
+template <bool STREAM>
+__device__ __forceinline__ u4r load16(const void* a) {
+  const u4r* v = static_cast<const u4r*>(a);
+  if constexpr (STREAM) return __builtin_nontemporal_load(v);
+  else return *v;
+}
+template <bool STREAM>
+__device__ __forceinline__ void store16(void* a, u4r x) {
+  u4r* v = static_cast<u4r*>(a);
+  if constexpr (STREAM) __builtin_nontemporal_store(x, v);
+  else *v = x;
+}
+
 // WIDE: units of E = 16 bytes of pairs (HALF: E channels of either half; INTERLEAVED: E/2
 // neighbouring pairs), then of E copied channels.  Otherwise a unit is one pair or one channel.
-template <int DT, bool IL, bool WIDE>
+template <int DT, bool IL, bool WIDE, bool STREAM>
 __global__ __launch_bounds__(256) void rope_kernel(const RopeParams p) {
   typedef Elem<DT> El;
   typedef typename El::raw raw;
@@ -80,7 +96,7 @@ __global__ __launch_bounds__(256) void rope_kernel(const RopeParams p) {
     for (int h = h0; h < h1; ++h) {
       const raw* a = x + (int64_t)h * p.xs_h + c;
       raw* z = o + (int64_t)h * p.os_h + c;
-      if constexpr (WIDE) *reinterpret_cast<u4r*>(z) = *reinterpret_cast<const u4r*>(a);
+      if constexpr (WIDE) store16<STREAM>(z, load16<STREAM>(a));
       else *z = *a;
     }
     return;
@@ -104,14 +120,14 @@ __global__ __launch_bounds__(256) void rope_kernel(const RopeParams p) {
 #pragma unroll 4
     for (int h = h0; h < h1; ++h) {
       V a, z;
-      a.v = *reinterpret_cast<const u4r*>(x + (int64_t)h * p.xs_h + u * E);
+      a.v = load16<STREAM>(x + (int64_t)h * p.xs_h + u * E);
 #pragma unroll
       for (int i = 0; i < NP; ++i) {
         const float e = El::load(a.r[2 * i]), f = El::load(a.r[2 * i + 1]);
         z.r[2 * i] = El::store(e * cs[i] - f * sn[i]);
         z.r[2 * i + 1] = El::store(f * cs[i] + e * sn[i]);
       }
-      *reinterpret_cast<u4r*>(o + (int64_t)h * p.os_h + u * E) = z.v;
+      store16<STREAM>(o + (int64_t)h * p.os_h + u * E, z.v);
     }
   } else {
     union V { u4r v; raw r[E]; };
@@ -120,8 +136,8 @@ __global__ __launch_bounds__(256) void rope_kernel(const RopeParams p) {
     for (int h = h0; h < h1; ++h) {
       const raw* xr = x + (int64_t)h * p.xs_h + u * E;
       V a, e, y, z;
-      a.v = *reinterpret_cast<const u4r*>(xr);
-      e.v = *reinterpret_cast<const u4r*>(xr + half);
+      a.v = load16<STREAM>(xr);
+      e.v = load16<STREAM>(xr + half);
 #pragma unroll
       for (int i = 0; i < NP; ++i) {
         const float f = El::load(a.r[i]), g = El::load(e.r[i]);
@@ -129,21 +145,23 @@ __global__ __launch_bounds__(256) void rope_kernel(const RopeParams p) {
         z.r[i] = El::store(g * cs[i] + f * sn[i]);
       }
       raw* orow = o + (int64_t)h * p.os_h + u * E;
-      *reinterpret_cast<u4r*>(orow) = y.v;
-      *reinterpret_cast<u4r*>(orow + half) = z.v;
+      store16<STREAM>(orow, y.v);
+      store16<STREAM>(orow + half, z.v);
     }
   }
 }
 
-template <int DT>
+template <int DT, bool IL>
 void launch(const RopeParams& p, bool wide, dim3 grid, hipStream_t st) {
-  if (wide) {
-    if (p.interleaved) hipLaunchKernelGGL((rope_kernel<DT, true, true>), grid, dim3(256), 0, st, p);
-    else hipLaunchKernelGGL((rope_kernel<DT, false, true>), grid, dim3(256), 0, st, p);
-  } else {
-    if (p.interleaved) hipLaunchKernelGGL((rope_kernel<DT, true, false>), grid, dim3(256), 0, st, p);
-    else hipLaunchKernelGGL((rope_kernel<DT, false, false>), grid, dim3(256), 0, st, p);
-  }
+  if (!wide) hipLaunchKernelGGL((rope_kernel<DT, IL, false, false>), grid, dim3(256), 0, st, p);
+  else if (p.streaming) hipLaunchKernelGGL((rope_kernel<DT, IL, true, true>), grid, dim3(256), 0, st, p);
+  else hipLaunchKernelGGL((rope_kernel<DT, IL, true, false>), grid, dim3(256), 0, st, p);
+}
+
+template <int DT>
+void launch_type(const RopeParams& p, bool wide, dim3 grid, hipStream_t st) {
+  if (p.interleaved) launch<DT, true>(p, wide, grid, st);
+  else launch<DT, false>(p, wide, grid, st);
 }
 
 }  // namespace
@@ -152,9 +170,9 @@ int launch_rope(const RopeParams& p, bool wide, void* stream) {
   const int64_t threads = p.tokens * p.head_groups * p.units;
   const dim3 grid((uint32_t)((threads + 255) / 256));
   hipStream_t st = static_cast<hipStream_t>(stream);
-  if (p.dtype == STARKV_DT_F32) launch<STARKV_DT_F32>(p, wide, grid, st);
-  else if (p.dtype == STARKV_DT_BF16) launch<STARKV_DT_BF16>(p, wide, grid, st);
-  else launch<STARKV_DT_F16>(p, wide, grid, st);
+  if (p.dtype == STARKV_DT_F32) launch_type<STARKV_DT_F32>(p, wide, grid, st);
+  else if (p.dtype == STARKV_DT_BF16) launch_type<STARKV_DT_BF16>(p, wide, grid, st);
+  else launch_type<STARKV_DT_F16>(p, wide, grid, st);
   return (int)hipGetLastError();
 }
 
