@@ -540,11 +540,13 @@ __device__ __forceinline__ u4 load_codes(const uint8_t* a) {
   else return *v;
 }
 
-// Up to 64 query rows of a KV head.  A workgroup's waves take 32-token steps in turn; with RG = 2
-// two row groups of 16 RT rows share the steps (a wave's state of 64 rows would leave one wave
-// per SIMD; the codes' second reader finds them in cache).
+// Up to 64 query rows of a KV head.  A workgroup's waves take 32-token steps in turn.  A wave holds
+// RT row tiles: one or two in 256 registers, so that two workgroups fit a compute unit; three in
+// the registers of a whole SIMD (40 rows: 75 us against 92 with two groups of two tiles, 2 x 64K
+// tokens of 8 heads).  Four tiles spill; there (RG = 2) two groups of two tiles share the steps,
+// and the codes' second reader finds them in cache (64 rows: 96 us against 132).
 template <int D, bool E4M3, int RT, int RG, bool SUMS>
-__global__ __launch_bounds__(256, 2) void dense_split_kernel(const DenseAttnParams p) {
+__global__ __launch_bounds__(256, RT >= 3 ? 1 : 2) void dense_split_kernel(const DenseAttnParams p) {
   constexpr int N = D / 64, CT = D / 16, NB = RT == 1 ? 3 : 2, TW = kWavesA / RG, kRound = 32 * TW;
   const int tid_lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int token_wave = wave / RG, row0 = wave % RG * (16 * RT), g = blockIdx.y;
@@ -652,19 +654,23 @@ __global__ __launch_bounds__(256, 2) void dense_split_kernel(const DenseAttnPara
     f4 sc[1][RT][2];
     float fk[1][RT][2];
 #pragma unroll
-    for (int a = 0; a < 2; ++a) {
+    for (int r = 0; r < RT; ++r) sc[0][r][0] = sc[0][r][1] = (f4){0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-      for (int r = 0; r < RT; ++r) sc[0][r][a] = (f4){0.0f, 0.0f, 0.0f, 0.0f};
+    for (int n = 0; n < N; ++n)
 #pragma unroll
-      for (int n = 0; n < N; ++n)
+      for (int h = 0; h < 2; ++h) {
+        h8 k[2];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const h8 k = code8<E4M3>(y.k[a][n][2 * h], y.k[a][n][2 * h + 1]);
+        for (int a = 0; a < 2; ++a) k[a] = code8<E4M3>(y.k[a][n][2 * h], y.k[a][n][2 * h + 1]);
 #pragma unroll
-          for (int r = 0; r < RT; ++r) sc[0][r][a] = mfma_f16(k, q[r][2 * n + h], sc[0][r][a]);
-        }
+        for (int r = 0; r < RT; ++r)
 #pragma unroll
-      for (int r = 0; r < RT; ++r) fk[0][r][a] = y.sk[a] * qs[r];
+          for (int a = 0; a < 2; ++a) sc[0][r][a] = mfma_f16(k[a], q[r][2 * n + h], sc[0][r][a]);
+      }
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+      fk[0][r][0] = y.sk[0] * qs[r];
+      fk[0][r][1] = y.sk[1] * qs[r];
     }
     float d[2], pr[RT][8];
     begin_steps<D, RT, 1>(s, sc, fk, lim, lim_lo, t, e8, y.lsv, quad, d);
@@ -1154,6 +1160,7 @@ template <int D, bool E4M3>
 void launch_rows(const DenseAttnParams& p, hipStream_t st) {
   if (p.rows <= 16) launch_split<D, E4M3, 1, 1>(p, st);
   else if (p.rows <= 32) launch_split<D, E4M3, 2, 1>(p, st);
+  else if (p.rows <= 48) launch_split<D, E4M3, 3, 1>(p, st);
   else if (p.rows <= kSplitRows) launch_split<D, E4M3, 2, 2>(p, st);
   else {
     const int tiles = (p.rows + kChunkRows - 1) / kChunkRows;

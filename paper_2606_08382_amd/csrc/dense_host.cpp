@@ -28,7 +28,10 @@ namespace {
 
 constexpr double kTwoPi = 6.283185307179586476925286766559;
 constexpr int kMaxDenseCtx = 524288;
-constexpr int kSplitTarget = 512;         // workgroups of a split pass: two per compute unit
+// Workgroups that an attention pass runs at a time: two per compute unit, one where 17 to 64 query
+// rows make a workgroup's start and end (queries, merge of its waves, partials) long (32 rows, 2 x
+// 64K tokens: 61 us against 67; 16 rows, 4 x 128K: 185 us against 164).
+int target_of(int64_t rows) { return rows > 16 && rows <= kSplitRows ? 256 : 512; }
 
 int64_t align256(int64_t x) { return (x + 255) / 256 * 256; }
 bool misaligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a != 0; }
@@ -357,17 +360,20 @@ starkv_status starkv_dense_read(const starkv_dense_plan* P, const void* cache,
 // ----------------------------------------------------------------------------- attention
 
 // Ranges of a pass over `rows` query rows per KV head.  Its workgroups (ranges x KV heads x row
-// tiles) run kSplitTarget at a time; the ranges are as many as one round takes, or, where a few
-// more make the last round fuller, up to four more (each range costs 2 % for its prologue and
-// partials).
+// tiles) run target_of() at a time.  The ranges are as many as one round takes, or, where a few
+// more make the last round fuller, up to four more (two, where one range fills a round: the
+// partials are large there); each costs 2 % for its start and partials.  From two rounds on the
+// row tiles are enough, and one range needs no partials.
 static int64_t split_ranges(const starkv_dense_plan* P, int64_t rows) {
   const int64_t tiles = rows <= kSplitRows ? 1 : (rows + kChunkRows - 1) / kChunkRows;
-  const int64_t per_range = P->cfg.n_kv_heads * tiles;
-  const int64_t one = std::max<int64_t>(kSplitTarget / per_range, 1);
+  const int64_t per_range = P->cfg.n_kv_heads * tiles, target = target_of(rows);
+  if (per_range >= 2 * target) return 1;
+  const int64_t one = std::max<int64_t>(target / per_range, 1);
+  const int64_t most = per_range >= target ? 3 : one + 4;
   int64_t best = one;
   double least = 1e30;
-  for (int64_t r = one; r <= one + 4; ++r) {
-    const double rounds = (double)((r * per_range + kSplitTarget - 1) / kSplitTarget);
+  for (int64_t r = one; r <= most; ++r) {
+    const double rounds = (double)((r * per_range + target - 1) / target);
     const double cost = rounds / r * (1.0 + 0.02 * (r - one));
     if (cost < least) {
       least = cost;
@@ -402,15 +408,18 @@ size_t starkv_dense_workspace_bytes(const starkv_dense_plan* P, int32_t n_q, int
                                     int32_t with_weights) {
   if (!P || n_q < 1 || max_ctx < 1) return 0;
   // Fewer query tokens may take more ranges: the largest need lies at n_q or just before a step
-  // of the row tiles.
+  // of the rows that the rule goes by.
   const int G = P->cfg.n_q_heads / P->cfg.n_kv_heads;
   const int gather = with_weights ? std::min(n_q, std::max(kSplitRows / G, 1)) : 0;
   int64_t need = workspace_of(P, n_q, max_ctx, false).total;
-  for (int64_t rows = kSplitRows; rows <= (int64_t)kSplitTarget * kChunkRows;
-       rows += rows < kChunkRows ? kChunkRows - rows : kChunkRows) {
+  for (int64_t rows = 16; rows <= 2 * 512 * (int64_t)kChunkRows;
+       rows += rows < kSplitRows ? kSplitRows - rows : rows < kChunkRows ? kChunkRows - rows : kChunkRows) {
     const int64_t n = rows / G;
     if (n >= n_q) break;
-    if (n >= 1) need = std::max(need, workspace_of(P, (int32_t)n, max_ctx, false).total);
+    if (n >= 1) {
+      need = std::max(need, workspace_of(P, (int32_t)n, max_ctx, false).total);
+      if (n < gather) need = std::max(need, workspace_of(P, (int32_t)n, max_ctx, true).total);
+    }
   }
   if (gather) need = std::max(need, workspace_of(P, gather, max_ctx, true).total);
   return (size_t)need;
