@@ -463,7 +463,7 @@ typedef struct {
   int32_t block_tokens;   /* T: 16, 32, 64 or 128 */
   int32_t dtype;          /* starkv_dtype of keys, values, queries and outputs: F16 or BF16 */
   int32_t n_blocks;       /* blocks in the pool, n_blocks * T < 2^31 */
-  double  softmax_scale;  /* > 0, or 0 for 1/sqrt(d) */
+  double  softmax_scale;  /* > 0 (at most 1e38), or 0 for 1/sqrt(d) */
   /* device int32 [B][H_kv][J], 4-byte aligned.  The pointer is fixed at plan creation, the
    * contents are read by every call at its place in the stream, and starkv_dense_evict may
    * rewrite them.  Append drops blocks whose entry is outside [0, n_blocks); the other
@@ -566,7 +566,9 @@ starkv_status starkv_dense_attn(const starkv_dense_plan* plan, const void* cache
  *   weights_out  device float [B][H_kv][J]: the kept blocks' weights, that of the unfinished
  *                block as entry n', then zeros.  NULL: weights, in place.
  *   ctx_out      device int32 [B]: ctx_len - (n - n') T.  May be ctx_len_dev (or NULL, the same).
- * Outputs that are not in place must not overlap inputs.  Positions of later tokens (for
+ * Outputs that are not in place must not overlap inputs.  The sequence's next finished blocks go
+ * into those that left: where one is shared with another sequence the caller gives its entry
+ * another pool block first.  Positions of later tokens (for
  * starkv_rope) count on from the unshortened sequence; lengths, and positions of
  * starkv_dense_append, from ctx_out.
  * Errors: INVALID_ARG, ALIGNMENT, HIP. */

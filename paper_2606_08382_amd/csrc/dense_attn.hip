@@ -279,9 +279,8 @@ __device__ __forceinline__ void begin_steps(State<D, RT>& s, f4 (&sc)[ST][RT][2]
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const int tok = first + st * 32 + a * 16 + e;
-            // (a NaN scale is moved to the scores of the tokens that are seen)
-            const float x = __builtin_fmaf(sc[st][r][a][e], fk[st][r][a], lsv[st * 2 + a] * 0.0f);
-            sc[st][r][a][e] = tok < lim[r] && tok < end ? x : -__builtin_inff();
+            sc[st][r][a][e] = tok < lim[r] && tok < end ? sc[st][r][a][e] * fk[st][r][a]
+                                                         : -__builtin_inff();
           }
           fk[st][r][a] = 1.0f;
         }
@@ -304,21 +303,16 @@ __device__ __forceinline__ void begin_steps(State<D, RT>& s, f4 (&sc)[ST][RT][2]
   }
   if (__any(over)) raise(s, top, most);
 #pragma unroll
-  for (int i = 0; i < 2 * ST; ++i) {
-    d[i] = lsv[i] - s.lv;
-    d[i] = d[i] < -40.0f || (masked && d[i] != d[i]) ? -40.0f : d[i];
-  }
+  for (int i = 0; i < 2 * ST; ++i) d[i] = fmaxf(lsv[i] - s.lv, -40.0f);
 }
 
-template <int D, int RT, bool SUMS>
+enum { kPlain, kSubSums, kNoSums };   // sums of finish_step: for l; also of subtiles; none (the caller's)
+template <int D, int RT, int SUMS>
 __device__ __forceinline__ void finish_step(State<D, RT>& s, const f4 (&sc)[RT][2],
                                             const float (&fk)[RT][2], const float* d, int t, int end,
                                             int col, int quad, const SubSums& sums,
                                             float (&pr)[RT][8]) {
-  // (a NaN scale makes NaN of its tokens' probabilities, and of nothing else)
-  float back[2];
-#pragma unroll
-  for (int a = 0; a < 2; ++a) back[a] = d[a] == d[a] ? exp2_fast(-d[a]) : 1.0f;
+  const float back[2] = {exp2_fast(-d[0]), exp2_fast(-d[1])};
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
     // a column that has seen nothing keeps reference -inf: x - 0 is -inf, its exponential 0
@@ -328,9 +322,10 @@ __device__ __forceinline__ void finish_step(State<D, RT>& s, const f4 (&sc)[RT][
       const float c = d[a] - m;
 #pragma unroll
       for (int e = 0; e < 4; ++e) pr[r][a * 4 + e] = exp2_fast(__builtin_fmaf(sc[r][a][e], fk[r][a], c));
+      if constexpr (SUMS == kNoSums) continue;
       const float part = (pr[r][a * 4] + pr[r][a * 4 + 1]) + (pr[r][a * 4 + 2] + pr[r][a * 4 + 3]);
       s.l[r] = __builtin_fmaf(part, back[a], s.l[r]);
-      if constexpr (SUMS) {
+      if constexpr (SUMS == kSubSums) {
         const float y = quad_sum(part) * back[a];
         const int row = sums.row0 + r * 16 + col;
         if (quad == 0 && row < sums.rows && t + a * 16 < end)
@@ -348,10 +343,12 @@ __device__ __forceinline__ void to_operand(const float (&pr)[RT][8], h8 (&ph)[RT
     for (int e = 0; e < 8; ++e) ph[r][e] = (_Float16)pr[r][e];
 }
 
-// log2 of a block's value scale (of a block of zeros: the smallest reference; NaN stays).
+// log2 of a block's value scale (of a block of zeros: the smallest reference).  A NaN value scale is
+// carried by the key scale: it makes NaN of the scores, and is masked with them.
 __device__ __forceinline__ float log_scale(float sv) {
-  return sv < 0x1p-100f ? kTinyScale : __builtin_amdgcn_logf(sv);
+  return sv >= 0x1p-100f ? __builtin_amdgcn_logf(sv) : kTinyScale;
 }
+__device__ __forceinline__ float key_scale(float sk, float sv) { return sv == sv ? sk : sv; }
 
 // Query rows row0 + 16 r + col, channels i*64 + quad*16 + h*8 + e (operand n = 2 i + h), as given.
 union Raw {
@@ -449,7 +446,7 @@ __device__ __forceinline__ void unfinished_block(const DenseAttnParams& p, State
     const float lsv[2] = {0.0f, 0.0f};
     float d[2], pr[RT][8];
     begin_steps<D, RT, 1>(s, sc, fk, lim, lim_lo, t, ctx, lsv, quad, d);
-    finish_step<D, RT, SUMS>(s, sc[0], fk[0], d, t, ctx, col, quad, sums, pr);
+    finish_step<D, RT, SUMS ? kSubSums : kPlain>(s, sc[0], fk[0], d, t, ctx, col, quad, sums, pr);
     u4 pa[RT], pb[RT];                              // fp16; or two bf16 parts
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
@@ -605,7 +602,8 @@ __global__ __launch_bounds__(256, RT >= 3 ? 1 : 2) void dense_split_kernel(const
     const int t = entry_token(i0);
     e = min(max(e, 0), p.c.n_blocks - 1);
     const Pair sc = p.c.scales[e];
-    return Entry{((uint32_t)e << (sh - 3)) + ((uint32_t)(t & (T - 1)) >> 4), sc.x, log_scale(sc.y)};
+    return Entry{((uint32_t)e << (sh - 3)) + ((uint32_t)(t & (T - 1)) >> 4), key_scale(sc.x, sc.y),
+                     log_scale(sc.y)};
   };
   const uint32_t v_sub = (uint32_t)T >> 4;          // from a key subtile to its value subtile
   auto load = [&](Tile<D>& x, const Entry& en, int i) {
@@ -674,7 +672,7 @@ __global__ __launch_bounds__(256, RT >= 3 ? 1 : 2) void dense_split_kernel(const
     }
     float d[2], pr[RT][8];
     begin_steps<D, RT, 1>(s, sc, fk, lim, lim_lo, t, e8, y.lsv, quad, d);
-    finish_step<D, RT, SUMS>(s, sc[0], fk[0], d, t, e8, col, quad, sums, pr);
+    finish_step<D, RT, SUMS ? kSubSums : kPlain>(s, sc[0], fk[0], d, t, e8, col, quad, sums, pr);
     h8 ph[RT];
     to_operand<RT>(pr, ph);
 #pragma unroll
@@ -840,6 +838,10 @@ __global__ __launch_bounds__(256, 2) void dense_chunk_kernel(const DenseAttnPara
       State<D, RT> s;
       reset(s);
       const SubSums none = {nullptr, 0, 0};
+      // row i of the first factor: ones over subtile i / 8's tokens (its lane: row col)
+      h8 ones;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) ones[e] = (e < 4) == (col < 8) ? (_Float16)1.0f : (_Float16)0.0f;
 
       const int e8 = min(min(t1, full), (sees + 15) & ~15);
       const int n = e8 > t0 ? (e8 - t0 + kTile - 1) / kTile : 0;
@@ -850,7 +852,8 @@ __global__ __launch_bounds__(256, 2) void dense_chunk_kernel(const DenseAttnPara
         const int t = max(min(t0 + i0 * kTile + lane * 16, e8 - 16), 0);
         const int e = min(max(table[t >> sh], 0), p.c.n_blocks - 1);
         const Pair sc = p.c.scales[e];
-        return Entry{((uint32_t)e << (sh - 3)) + ((uint32_t)(t & (T - 1)) >> 4), sc.x, log_scale(sc.y)};
+        return Entry{((uint32_t)e << (sh - 3)) + ((uint32_t)(t & (T - 1)) >> 4), key_scale(sc.x, sc.y),
+                     log_scale(sc.y)};
       };
       const uint32_t v_sub = (uint32_t)T >> 4;
       // A thread's codes of a tile: key units tid + 256 i (subtile, then 16-byte unit); value units of
@@ -944,9 +947,31 @@ __global__ __launch_bounds__(256, 2) void dense_chunk_kernel(const DenseAttnPara
 #pragma unroll
         for (int st = 0; st < 2; ++st) {
           float pr[RT][8];
-          finish_step<D, RT, false>(s, sc[st], fk[st], d + 2 * st, t, e8, col, quad, none, pr);
+          finish_step<D, RT, kNoSums>(s, sc[st], fk[st], d + 2 * st, t, e8, col, quad, none, pr);
           h8 ph[RT];
           to_operand<RT>(pr, ph);
+          // The sums by one more product, of rows that are one over a subtile's tokens: the lanes of
+          // quads 0 and 1 get the first subtile's sum, the others the second's (each twice).  Where
+          // the value scales make the operand small, fp16 would drop tokens from the sums: added
+          // in fp32 (twice, as above).
+          const float d0 = d[2 * st], d1 = d[2 * st + 1];
+          const float low = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(fminf(d0, d1))));
+          if (low >= -4.0f) {
+            const float back = exp2_fast(-(quad < 2 ? d0 : d1));
+#pragma unroll
+            for (int r = 0; r < RT; ++r) {
+              const f4 sum = mfma_f16(ones, ph[r], (f4){0.0f, 0.0f, 0.0f, 0.0f});
+              s.l[r] = __builtin_fmaf(sum[0], back, s.l[r]);
+            }
+          } else {
+            const float b0 = 2.0f * exp2_fast(-d0), b1 = 2.0f * exp2_fast(-d1);
+#pragma unroll
+            for (int r = 0; r < RT; ++r) {
+              const float x = (pr[r][0] + pr[r][1]) + (pr[r][2] + pr[r][3]);
+              const float y = (pr[r][4] + pr[r][5]) + (pr[r][6] + pr[r][7]);
+              s.l[r] = __builtin_fmaf(y, b1, __builtin_fmaf(x, b0, s.l[r]));
+            }
+          }
 #pragma unroll
           for (int c = 0; c < CT; ++c) {
             const h8 vf = *reinterpret_cast<const h8*>(buf + kKeys + (st * CT + c) * kFrag + lane * 16);
@@ -956,6 +981,8 @@ __global__ __launch_bounds__(256, 2) void dense_chunk_kernel(const DenseAttnPara
         }
         __syncthreads();
       }
+#pragma unroll
+      for (int r = 0; r < RT; ++r) s.l[r] *= 0.5f;
       if (full < t1 && sees > full)
         unfinished_block<D, RT, false>(p, s, b, g, ctx, min(ctx, sees), full, 32, row0, lim, lim_lo, none,
                                        fresh(lane));

@@ -28,10 +28,11 @@ namespace {
 
 constexpr double kTwoPi = 6.283185307179586476925286766559;
 constexpr int kMaxDenseCtx = 524288;
-// Workgroups that an attention pass runs at a time: two per compute unit, one where 17 to 64 query
-// rows make a workgroup's start and end (queries, merge of its waves, partials) long (32 rows, 2 x
-// 64K tokens: 61 us against 67; 16 rows, 4 x 128K: 185 us against 164).
-int target_of(int64_t rows) { return rows > 16 && rows <= kSplitRows ? 256 : 512; }
+// Workgroups that an attention pass runs at a time: one per compute unit for the split kernel, whose
+// workgroup's start and end (queries, merge of its waves, partials) cost more than a second one in
+// flight gains (with two: 32 ragged sequences 128 us against 121, 32 query rows 67 against 61,
+// 4 x 128K the same 164); two for the chunk kernel.
+int target_of(int64_t rows) { return rows <= kSplitRows ? 256 : 512; }
 
 int64_t align256(int64_t x) { return (x + 255) / 256 * 256; }
 bool misaligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a != 0; }
@@ -214,8 +215,8 @@ starkv_status starkv_dense_plan_create(const starkv_dense_config* c, starkv_dens
   if (T != 16 && T != 32 && T != 64 && T != 128)
     return fail_with(STARKV_ERR_INVALID_ARG, "block_tokens %d not 16, 32, 64 or 128", T);
   if (c->n_blocks < 1) return fail_with(STARKV_ERR_INVALID_ARG, "n_blocks %d < 1", c->n_blocks);
-  if (!(c->softmax_scale >= 0.0) || !std::isfinite(c->softmax_scale))
-    return fail_with(STARKV_ERR_INVALID_ARG, "softmax_scale must be finite and positive, or 0");
+  if (!(c->softmax_scale >= 0.0) || c->softmax_scale > 1e38)
+    return fail_with(STARKV_ERR_INVALID_ARG, "softmax_scale must be positive and at most 1e38, or 0");
   if (!c->block_table) return fail_with(STARKV_ERR_INVALID_ARG, "block_table is NULL");
   if (misaligned(c->block_table, 4))
     return fail_with(STARKV_ERR_ALIGNMENT, "block_table not 4-byte aligned");

@@ -404,7 +404,9 @@ def reference(k, v, q, ctx, q_len, code, T, scale=None):
             for i in range(g * G, (g + 1) * G):
                 o, a, big, p = R.attend(q[b, :m, i], K, V, c, L - m)
                 out[b, :m, i] = o
-                rel = 2.0 ** -11 + 4 * big * (d + 8) * 2.0 ** -24 + 2.0 ** -24 * (L / 16 + 64)
+                # (above 64 rows the sum that divides is of the rounded probabilities too: each
+                # moves the quotient by up to its own 2^-11 of |v - out|, at most twice sum p |v|)
+                rel = 2.0 ** -11 * (2 if n * G > 64 else 1) + 4 * big * (d + 8) * 2.0 ** -24 + 2.0 ** -24 * (L / 16 + 64)
                 # (a block that is not finite has no part in the rows that are compared)
                 top = torch.nan_to_num(V.abs(), nan=0.0).amax() * L * 2.0 ** -29 if L else 0.0
                 tol[b, :m, i] = eps / 2 * o.abs() + (1 + eps) * (rel[:, None] * a + top) + 2.0 ** -25
@@ -497,22 +499,29 @@ def test_many_query_rows_need_no_partials():
     assert torch.equal(odd[..., 1:], out) and (odd[..., 0] == 3).all()
 
 
-def test_large_scores_and_scales():
-    run_attend([700, 130], k_scale=40.0)                     # one token takes nearly all
-    run_attend([700, 130], k_scale=3000.0, dtype="bf16", code=1)
-    run_attend([700, 130], k_scale=1e-30)
-    run_attend([300, 64], scale=2.5, dtype="f16")
+@pytest.mark.parametrize("n", [1, 4, 10, 15, 45])           # 4, 16, 40, 60 and 180 rows of a KV head
+def test_large_scores_and_scales(n):
+    run_attend([700, 130], n=n, k_scale=40.0)                # one token takes nearly all
+    run_attend([700, 130], n=n, k_scale=3000.0, dtype="bf16", code=1)
+    run_attend([700, 130], n=n, k_scale=1e-30)
+    run_attend([300, 64], n=n, scale=2.5, dtype="f16")
 
     def uneven(k, v):                                        # value scales 2^-60 .. 2^60
         for j in range(0, v.shape[1], 64):
             v[:, j:j + 64] = (v[:, j:j + 64].double() * 2.0 ** ((j // 64 * 37) % 121 - 60)).bfloat16()
-    run_attend([900, 450], edit=uneven)
+    run_attend([900, 450], n=n, edit=uneven)
+
+    def falling(k, v):                                       # a large block first, then small ones
+        v[:, 64:] = (v[:, 64:].double() / 100).to(v.dtype)
+    run_attend([900, 450], n=n, edit=falling)
+    run_attend([900, 450], n=n, edit=falling, code=1, T=16, d=64, dtype="f16")
 
     def zeros(k, v):
         v[:, :128] = 0
         k[:, 64:192] = 0
-    run_attend([300, 200], edit=zeros)
-    run_attend([300, 200], edit=lambda k, v: v.zero_(), code=1)
+    run_attend([300, 200], n=n, edit=zeros)
+    run_attend([300, 200], n=n, edit=lambda k, v: v[:, 128:].zero_())
+    run_attend([300, 200], n=n, edit=lambda k, v: v.zero_(), code=1)
 
 
 def test_query_extremes():
