@@ -84,7 +84,7 @@ struct DenseAttnParams {
   Pair* part_ml;                            // [slot][H_kv][rows]: (reference, sum)
   Pair* sub;                                // [B*H_kv][subtile][rows]: (sum, reference)
   int32_t n_q, group, rows;                     // rows = n_q * group
-  int32_t max_ctx, ranges, sub_per_head;
+  int32_t max_ctx, ranges, min_units, sub_per_head;   // min_units: of a range
   int32_t q_wide, out_wide;                     // query rows 16-, output rows 8-byte aligned
   float scale_log2;                             // softmax scale * log2(e)
 };

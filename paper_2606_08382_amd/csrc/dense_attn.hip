@@ -145,7 +145,7 @@ __device__ __forceinline__ int range_units(const DenseAttnParams& p, const Lens&
     const int b = b0 + lane;
     sum += __builtin_amdgcn_readlane(wave_scan(b < p.c.batch ? units_of(clamp_ctx(p, b)) : 0), 63);
   }
-  return max((int)(((uint32_t)sum + (uint32_t)p.ranges - 1) / (uint32_t)p.ranges), 1);
+  return max((int)(((uint32_t)sum + (uint32_t)p.ranges - 1) / (uint32_t)p.ranges), p.min_units);
 }
 
 // The sequence that holds unit `at`, its length and its first unit; false past the last.
@@ -1128,8 +1128,9 @@ __global__ __launch_bounds__(256) void dense_combine_kernel(const DenseAttnParam
   }
 }
 
-// The same for the chunk kernel's many rows and few parts: a wave takes four rows at once.  With one
-// range the rows are written already, but for sequences without tokens.
+// The same for the chunk kernel's many rows: a wave takes four rows at once, sixteen lanes a row for
+// the parts' references and sums.  With one range the rows are written already, but for
+// sequences without tokens.
 template <int D>
 __global__ __launch_bounds__(256) void dense_combine_rows_kernel(const DenseAttnParams p) {
   constexpr int C = D / 64, K = 4;
@@ -1138,38 +1139,47 @@ __global__ __launch_bounds__(256) void dense_combine_rows_kernel(const DenseAttn
   int first, count, ctx;
   slots_of(p, b, lane, &first, &count, &ctx);
   if ((p.ranges == 1 && count > 0) || row0 >= p.rows) return;
-  const int n = min(K, p.rows - row0);
+  const int n = min(K, p.rows - row0), i16 = lane & 15;
   const int64_t step = (int64_t)p.c.n_kv * p.rows;
   const int64_t slot0 = ((int64_t)first * p.c.n_kv + g) * p.rows + row0;
-  float m[K], l[K] = {}, o[K][C] = {};
+  const Pair* ml = p.part_ml + slot0 + min(lane >> 4, n - 1);
+  auto part = [&](int i) { return i < count ? ml[i * step] : Pair{-__builtin_inff(), 0.0f}; };
+  const Pair head = part(i16);
+  float m = head.x;
+  for (int i = 16 + i16; i < count; i += 16) m = fmaxf(m, ml[i * step].x);
 #pragma unroll
-  for (int r = 0; r < K; ++r) m[r] = -__builtin_inff();
-  for (int i = 0; i < count; ++i)
+  for (int o = 1; o < 16; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
+  float l = 0.0f, o[K][C] = {};
+  for (int i0 = 0; i0 < count; i0 += 16) {
+    const Pair x = i0 ? part(i0 + i16) : head;
+    const float f = x.x == m ? x.y : x.y * exp2_fast(x.x - m);
+    l += f;
+    const int most = min(16, count - i0);
+#pragma unroll 4
+    for (int u = 0; u < most; ++u)
 #pragma unroll
-    for (int r = 0; r < K; ++r) m[r] = fmaxf(m[r], p.part_ml[slot0 + i * step + min(r, n - 1)].x);
-#pragma unroll 2
-  for (int i = 0; i < count; ++i)
+      for (int r = 0; r < K; ++r) {
+        const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), r * 16 + u));
+        const int64_t slot = slot0 + (i0 + u) * step + min(r, n - 1);
 #pragma unroll
-    for (int r = 0; r < K; ++r) {
-      const int64_t slot = slot0 + i * step + min(r, n - 1);
-      const Pair ml = p.part_ml[slot];
-      const float f = ml.x == m[r] ? ml.y : ml.y * exp2_fast(ml.x - m[r]);
-      l[r] += f;
-#pragma unroll
-      for (int c = 0; c < C; ++c) {
-        const float v = p.part_o[slot * D + lane * C + c];
-        o[r][c] += f == 0.0f ? 0.0f : f * v;
+        for (int c = 0; c < C; ++c) {
+          const float v = p.part_o[slot * D + lane * C + c];
+          o[r][c] += w == 0.0f ? 0.0f : w * v;
+        }
       }
-    }
+  }
+#pragma unroll
+  for (int x = 1; x < 16; x <<= 1) l += __shfl_xor(l, x);
 #pragma unroll
   for (int r = 0; r < K; ++r) {
     const int row = row0 + r;
+    const float lr = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(l), r * 16));
     if (row_limit(p, b, ctx, row) < 0) continue;
     const int jq = row / p.group, iq = row % p.group;
     uint16_t* out = p.out + b * p.os_b + jq * p.os_t + (g * p.group + iq) * p.os_h + lane * C;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      const float v = l[r] == 0.0f ? 0.0f : o[r][c] / l[r];
+      const float v = lr == 0.0f ? 0.0f : o[r][c] / lr;
       out[c] = p.c.bf16 ? __builtin_bit_cast(uint16_t, (__bf16)v)
                         : __builtin_bit_cast(uint16_t, (_Float16)v);
     }
