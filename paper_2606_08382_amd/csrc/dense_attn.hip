@@ -916,13 +916,6 @@ __global__ __launch_bounds__(256, 2) void dense_chunk_kernel(const DenseAttnPara
           sk[k] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(now.sk), l));
           lsv[k] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(now.lsv), l));
         }
-        if (i + 1 < n) store(lds[(i + 1) & 1]);
-        if (((i + 1) & 15) == 0) {
-          now = next;
-          next = entries(i + 17);
-        }
-        // (tile i + 2 lies in the next 16 when i + 1 ends these)
-        if (i + 2 < n) load(((i + 2) & 15) == 0 ? next : now, i + 2);
         const uint8_t* buf = lds[i & 1];
         const int t = t0 + i * kTile;
         // both steps' scores first: the second's exponentials run beside the first's products
@@ -979,6 +972,14 @@ __global__ __launch_bounds__(256, 2) void dense_chunk_kernel(const DenseAttnPara
             for (int r = 0; r < RT; ++r) s.o[r][c] = mfma_f16(vf, ph[r], s.o[r][c]);
           }
         }
+        // the next tile's codes, in registers since the last one, and the loads of the one after
+        if (i + 1 < n) store(lds[(i + 1) & 1]);
+        if (((i + 1) & 15) == 0) {
+          now = next;
+          next = entries(i + 17);
+        }
+        // (tile i + 2 lies in the next 16 when i + 1 ends these)
+        if (i + 2 < n) load(((i + 2) & 15) == 0 ? next : now, i + 2);
         __syncthreads();
       }
 #pragma unroll
