@@ -543,7 +543,9 @@ size_t        starkv_dense_workspace_bytes(const starkv_dense_plan* plan, int32_
  *   ws           device, starkv_dense_workspace_bytes(plan, n_q, max_ctx, weights != NULL)
  *                bytes, 256-byte aligned.
  * Scores, softmax sums and accumulators are fp32; probabilities enter the product with the
- * values in fp16 (with two bf16 parts for the unfinished block of a BF16 plan).
+ * values in fp16 (with two bf16 parts for the unfinished block of a BF16 plan), relative to the
+ * largest score and the largest value scale that a wave has met: products below 2^-30 of these
+ * are dropped.
  * Errors: INVALID_ARG, UNSUPPORTED, CAPACITY, WORKSPACE, ALIGNMENT, HIP. */
 starkv_status starkv_dense_attn(const starkv_dense_plan* plan, const void* cache, const void* q,
                                 const starkv_strides* qs, int32_t n_q, const int32_t* q_len_dev,

@@ -72,6 +72,11 @@ struct DenseEvictParams {
   int32_t keep, sink, recent;
 };
 
+// A sequence's parts in the partials of an attention pass.
+struct Slots {
+  int32_t first, count, ctx, pad;
+};
+
 struct DenseAttnParams {
   DenseCache c;
   const uint16_t* q;
@@ -80,6 +85,7 @@ struct DenseAttnParams {
   const int32_t* q_len;
   const int32_t* ctx_len;
   float* weights;
+  Slots* slots;                                 // [B]
   float* part_o;                                // [slot][H_kv][rows][d], normalized
   Pair* part_ml;                            // [slot][H_kv][rows]: (reference, sum)
   Pair* sub;                                // [B*H_kv][subtile][rows]: (sum, reference)

@@ -171,23 +171,22 @@ __device__ __forceinline__ bool find_unit(const DenseAttnParams& p, const Lens& 
     x.incl = before + wave_scan(units_of(x.ctx));
   }
 }
-// First slot and number of slots of sequence b, and its length.
-__device__ __forceinline__ void slots_of(const DenseAttnParams& p, int b, int lane, int* first,
-                                         int* count, int* ctx) {
-  const Lens ls = first_lens(p, lane);
-  const uint32_t R = range_units(p, ls, lane);
+// Leaves every sequence's first slot, number of slots and length for the combine pass, which would
+// otherwise walk over the batch once per row.  By one wave of the first workgroup.
+__device__ __forceinline__ void write_slots(const DenseAttnParams& p, const Lens& ls, int R, int lane) {
   Lens x = ls;
-  int before = 0;
-  for (int b0 = 64; b0 <= b; b0 += 64) {
+  uint32_t before = 0;
+  for (int b0 = 0; b0 < p.c.batch; b0 += 64) {
+    const int b = b0 + lane;
+    if (b0) {
+      x.ctx = b < p.c.batch ? clamp_ctx(p, b) : 0;
+      x.incl = wave_scan(units_of(x.ctx));
+    }
+    const uint32_t u = units_of(x.ctx), start = before + x.incl - u, r = R;
+    if (b < p.c.batch)
+      p.slots[b] = {(int)(start / r) + b, u ? (int)((start + u - 1) / r - start / r) + 1 : 0, x.ctx, 0};
     before += __builtin_amdgcn_readlane(x.incl, 63);
-    x.ctx = b0 + lane < p.c.batch ? clamp_ctx(p, b0 + lane) : 0;
-    x.incl = wave_scan(units_of(x.ctx));
   }
-  *ctx = __builtin_amdgcn_readlane(x.ctx, b & 63);
-  const uint32_t u = units_of(*ctx);
-  const uint32_t start = before + __builtin_amdgcn_readlane(x.incl, b & 63) - u;
-  *first = start / R + b;
-  *count = u > 0 ? (start + u - 1) / R - start / R + 1 : 0;
 }
 
 // Tokens that query row r (query token r / group) of sequence b sees: at most ctx; 0: none;
@@ -552,6 +551,7 @@ __global__ __launch_bounds__(256, RT >= 3 ? 1 : 2) void dense_split_kernel(const
   __shared__ float so[kWavesA][16][D + 4];
   __shared__ float sm[kWavesA][RT * 16], sl[kWavesA][RT * 16];
   const int sh = p.c.shift, T = 1 << sh;
+  if (blockIdx.x == 0 && blockIdx.y == 0 && wave == 0) write_slots(p, lens, R, tid_lane);
   Place pl;
   int at = blockIdx.x * R;
   const int at_end = at + R;
@@ -804,6 +804,7 @@ __global__ __launch_bounds__(256, 2) void dense_chunk_kernel(const DenseAttnPara
   const int sh = p.c.shift, T = 1 << sh;
   const Lens lens = first_lens(p, lane);
   const int R = range_units(p, lens, lane);
+  if (blockIdx.x == 0 && wave == 0) write_slots(p, lens, R, lane);
   Place pl;
   int at = range * R;
   const int at_end = at + R;
@@ -1059,8 +1060,8 @@ __device__ __forceinline__ Merged merge_row(const DenseAttnParams& p, int first,
 __device__ __forceinline__ void gather_weights(const DenseAttnParams& p, int tile, int g, int b,
                                                float* sM, float* sI) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int first, count, ctx;
-  slots_of(p, b, lane, &first, &count, &ctx);
+  const Slots sl = p.slots[b];
+  const int first = sl.first, count = sl.count, ctx = sl.ctx;
   const int64_t head = (int64_t)b * p.c.n_kv + g;
   const int sub_shift = p.c.shift - 4, subs = (ctx + 15) >> 4;
   if (tile * (256 << sub_shift) >= subs) return;
@@ -1101,8 +1102,8 @@ __global__ __launch_bounds__(256) void dense_combine_kernel(const DenseAttnParam
     gather_weights(p, row - p.rows, g, b, sM, sI);
     return;
   }
-  int first, count, ctx;
-  slots_of(p, b, lane, &first, &count, &ctx);
+  const Slots sl = p.slots[b];
+  const int first = sl.first, count = sl.count, ctx = sl.ctx;
   if (row_limit(p, b, ctx, row) < 0) return;
   const Merged t = merge_row(p, first, count, g, row, lane);
   float o[C] = {};
@@ -1139,8 +1140,8 @@ __global__ __launch_bounds__(256) void dense_combine_rows_kernel(const DenseAttn
   constexpr int C = D / 64, K = 4;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = blockIdx.y, b = blockIdx.z, row0 = (blockIdx.x * 4 + wave) * K;
-  int first, count, ctx;
-  slots_of(p, b, lane, &first, &count, &ctx);
+  const Slots sl = p.slots[b];
+  const int first = sl.first, count = sl.count, ctx = sl.ctx;
   if ((p.ranges == 1 && count > 0) || row0 >= p.rows) return;
   const int n = min(K, p.rows - row0), i16 = lane & 15;
   const int64_t step = (int64_t)p.c.n_kv * p.rows;

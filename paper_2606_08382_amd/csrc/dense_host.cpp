@@ -386,7 +386,7 @@ static int64_t split_ranges(const starkv_dense_plan* P, int64_t rows) {
 
 struct DenseWorkspace {
   int64_t ranges;
-  int64_t ml, sub, total;             // offsets in bytes; the outputs' partials come first
+  int64_t part, ml, sub, total;       // offsets in bytes; the sequences' slots come first
   int32_t sub_per_head;
 };
 static DenseWorkspace workspace_of(const starkv_dense_plan* P, int32_t n_q, int32_t max_ctx,
@@ -398,7 +398,8 @@ static DenseWorkspace workspace_of(const starkv_dense_plan* P, int32_t n_q, int3
   // (the chunk kernel writes the output itself where one range holds all sequences)
   const bool whole = rows > kSplitRows && w.ranges == 1;
   const int64_t slots = whole ? 1 : (w.ranges + c.batch) * c.n_kv_heads * rows;
-  w.ml = align256(slots * c.head_dim * 4);
+  w.part = align256((int64_t)c.batch * sizeof(Slots));
+  w.ml = w.part + align256(slots * c.head_dim * 4);
   w.sub = w.ml + align256(slots * 8);
   w.sub_per_head = (max_ctx + 15) / 16;
   w.total = w.sub + (weights ? align256((int64_t)c.batch * c.n_kv_heads * w.sub_per_head * rows * 8) : 0);
@@ -469,7 +470,8 @@ starkv_status starkv_dense_attn(const starkv_dense_plan* P, const void* cache, c
   p.ctx_len = ctx_len_dev;
   p.weights = weights;
   uint8_t* base = static_cast<uint8_t*>(ws);
-  p.part_o = reinterpret_cast<float*>(base);
+  p.slots = reinterpret_cast<Slots*>(base);
+  p.part_o = reinterpret_cast<float*>(base + w.part);
   p.part_ml = reinterpret_cast<Pair*>(base + w.ml);
   p.sub = reinterpret_cast<Pair*>(base + w.sub);
   p.n_q = n_q;

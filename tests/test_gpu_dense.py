@@ -657,13 +657,15 @@ def test_offsets_beyond_32_bits():
     assert torch.equal(ks[0, :, 1].cpu(), R.cached(k[0, :, 1], 0, T).float())
 
 
-@pytest.mark.parametrize("B", [3, 70])
+@pytest.mark.parametrize("B", [3, 70, 300])
 def test_many_ragged_sequences_and_long_contexts(B):
     """Work items over ragged lengths: more than one wave's worth of sequences, long ones."""
     g = torch.Generator().manual_seed(B)
     ctx = torch.randint(0, 400, (B,), generator=g).tolist()
     ctx[1], ctx[-1] = 20000 if B == 3 else 3000, 0
     run_attend(ctx, n_q=4, n_kv=1, d=64, T=32, code=1)
+    if B == 300:
+        run_attend([min(c, 90) for c in ctx], n=67, n_q=1, n_kv=1, d=64, T=16, code=0)
 
 
 def test_same_bytes_again_and_from_other_streams():
