@@ -28,12 +28,6 @@ namespace {
 
 constexpr double kTwoPi = 6.283185307179586476925286766559;
 constexpr int kMaxDenseCtx = 524288;
-// Workgroups that an attention pass runs at a time: one per compute unit for the split kernel, whose
-// workgroup's start and end (queries, merge of its waves, partials) cost more than a second one in
-// flight gains (with two: 32 ragged sequences 128 us against 121, 32 query rows 67 against 61,
-// 4 x 128K the same 164); two for the chunk kernel.
-int target_of(int64_t rows) { return rows <= kSplitRows ? 256 : 512; }
-
 int64_t align256(int64_t x) { return (x + 255) / 256 * 256; }
 bool misaligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a != 0; }
 
@@ -360,6 +354,18 @@ starkv_status starkv_dense_read(const starkv_dense_plan* P, const void* cache,
 
 // ----------------------------------------------------------------------------- attention
 
+// Workgroups that an attention pass runs at a time.  The split kernel: one per compute unit, since a
+// workgroup's start and end (queries, merge of its waves, partials) cost more than a second one in
+// flight gains (with two: 32 ragged sequences of 8 KV heads 128 us against 121, 32 query rows 67
+// against 61, 4 x 128K the same 164); two where a range holds more than a sequence, so that one's
+// starts and ends run beside the other's stream (300 sequences of 200 to 600 tokens 124 us against
+// 165, 64 of 1000 to 3000 67 against 69), up to the two row tiles that fit twice.  The chunk
+// kernel: two.
+static int64_t target_of(const starkv_dense_plan* P, int64_t rows) {
+  if (rows > kSplitRows) return 512;
+  return rows <= 32 && (int64_t)P->cfg.batch * P->cfg.n_kv_heads > 256 ? 512 : 256;
+}
+
 // Ranges of a pass over `rows` query rows per KV head.  Its workgroups (ranges x KV heads x row
 // tiles) run target_of() at a time.  The ranges are as many as one round takes, or, where a few
 // more make the last round fuller, up to four more (two, where one range fills a round: the
@@ -367,7 +373,7 @@ starkv_status starkv_dense_read(const starkv_dense_plan* P, const void* cache,
 // row tiles are enough, and one range needs no partials.
 static int64_t split_ranges(const starkv_dense_plan* P, int64_t rows) {
   const int64_t tiles = rows <= kSplitRows ? 1 : (rows + kChunkRows - 1) / kChunkRows;
-  const int64_t per_range = P->cfg.n_kv_heads * tiles, target = target_of(rows);
+  const int64_t per_range = P->cfg.n_kv_heads * tiles, target = target_of(P, rows);
   if (per_range >= 2 * target) return 1;
   const int64_t one = std::max<int64_t>(target / per_range, 1);
   const int64_t most = per_range >= target ? 3 : one + 4;
@@ -414,8 +420,8 @@ size_t starkv_dense_workspace_bytes(const starkv_dense_plan* P, int32_t n_q, int
   const int G = P->cfg.n_q_heads / P->cfg.n_kv_heads;
   const int gather = with_weights ? std::min(n_q, std::max(kSplitRows / G, 1)) : 0;
   int64_t need = workspace_of(P, n_q, max_ctx, false).total;
-  for (int64_t rows = 16; rows <= 2 * 512 * (int64_t)kChunkRows;
-       rows += rows < kSplitRows ? kSplitRows - rows : rows < kChunkRows ? kChunkRows - rows : kChunkRows) {
+  for (int64_t rows = 32; rows <= 2 * 512 * (int64_t)kChunkRows;
+       rows += rows < kChunkRows ? rows : kChunkRows) {
     const int64_t n = rows / G;
     if (n >= n_q) break;
     if (n >= 1) {

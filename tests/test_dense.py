@@ -147,10 +147,11 @@ def test_dense_layout(d, T, cap, blocks):
     assert S.starkv_dense_cache_bytes(plan) == L.total_bytes
 
 
+@pytest.mark.parametrize("batch", [2, 40, 300])
 @pytest.mark.parametrize("heads", [(8, 8), (8, 1), (32, 8), (64, 1), (6, 2)])
-def test_workspace_serves_fewer_tokens_and_shorter_contexts(heads):
+def test_workspace_serves_fewer_tokens_and_shorter_contexts(heads, batch):
     plan = S.starkv_dense_plan_create(dense_cfg(n_q_heads=heads[0], n_kv_heads=heads[1],
-                                                capacity=5000))
+                                                capacity=5000, batch=batch))
     sizes = {(n, ctx, w): S.starkv_dense_workspace_bytes(plan, n, ctx, w)
              for n in (1, 2, 3, 5, 8, 16, 17, 33, 64, 200, 1000) for ctx in (1, 16, 17, 777, 5000)
              for w in (False, True)}
