@@ -557,201 +557,201 @@ __global__ __launch_bounds__(256, RT >= 3 ? 1 : 2) void dense_split_kernel(const
   const int at_end = at + R;
   if (!find_unit(p, lens, at, tid_lane, &pl)) return;
   for (;;) {                                       // the range's part of one sequence after another
-  // (a lane index that the compiler takes for new: addresses and masks are formed where they are
-  // used instead of being kept in registers over the whole range)
-  int lane = fresh(tid_lane);
-  int col = lane & 15, quad = lane >> 4;
-  struct { int b, ctx, t0, t1; } it;
-  it.b = pl.b;
-  it.ctx = pl.ctx;
-  it.t0 = (at - pl.start) * kUnit;
-  it.t1 = min(min(at_end - pl.start, units_of(pl.ctx)) * kUnit, pl.ctx);
-  const int full = it.ctx & ~(T - 1);
-  const int64_t head = (int64_t)it.b * p.c.n_kv + g;
-  const int e8 = min(it.t1, full), tw = it.t0 + 32 * token_wave;   // the wave's finished blocks
+    // (a lane index that the compiler takes for new: addresses and masks are formed where they are
+    // used instead of being kept in registers over the whole range)
+    int lane = fresh(tid_lane);
+    int col = lane & 15, quad = lane >> 4;
+    struct { int b, ctx, t0, t1; } it;
+    it.b = pl.b;
+    it.ctx = pl.ctx;
+    it.t0 = (at - pl.start) * kUnit;
+    it.t1 = min(min(at_end - pl.start, units_of(pl.ctx)) * kUnit, pl.ctx);
+    const int full = it.ctx & ~(T - 1);
+    const int64_t head = (int64_t)it.b * p.c.n_kv + g;
+    const int e8 = min(it.t1, full), tw = it.t0 + 32 * token_wave;   // the wave's finished blocks
 
-  // The chains of loads that a part begins with overlap: the table entries of the first 64 steps
-  // (a subtile per lane and 32 steps), the queries, then the entries' scales and codes.
-  const int32_t* table = p.c.table + head * p.c.blocks_per_head;
-  auto entry_token = [&](int i0) {
-    return max(min(tw + (i0 + (lane >> 1)) * kRound + (lane & 1) * 16, e8 - 16), 0);
-  };
-  const int entry0 = table[entry_token(0) >> sh], entry1 = table[entry_token(32) >> sh];
+    // The chains of loads that a part begins with overlap: the table entries of the first 64 steps
+    // (a subtile per lane and 32 steps), the queries, then the entries' scales and codes.
+    const int32_t* table = p.c.table + head * p.c.blocks_per_head;
+    auto entry_token = [&](int i0) {
+      return max(min(tw + (i0 + (lane >> 1)) * kRound + (lane & 1) * 16, e8 - 16), 0);
+    };
+    const int entry0 = table[entry_token(0) >> sh], entry1 = table[entry_token(32) >> sh];
 
-  // queries: row r of the tile in column `col`, channels i*64 + quad*16 + h*8 + e
-  h8 q[RT][2 * N];
-  float qs[RT];
-  int lim[RT];
-  int lm[RT];
-  int lim_lo = 0x7fffffff;
-#pragma unroll
-  for (int r = 0; r < RT; ++r) {
-    lm[r] = row_limit(p, it.b, it.ctx, row0 + r * 16 + col);
-    lim[r] = lm[r] < 0 ? 0x7fffffff : lm[r];       // rows without a query see everything
-    lim_lo = min(lim_lo, lim[r]);
-  }
-  Raw raw[RT][2 * N];
-  load_queries<D, RT>(p, it.b, g, row0, col, quad, lm, raw);
-#pragma unroll
-  for (int o = 8; o >= 1; o >>= 1) lim_lo = min(lim_lo, __shfl_xor(lim_lo, o));
-  lim_lo = __builtin_amdgcn_readfirstlane(lim_lo);
-
-  const int steps = e8 > tw ? (e8 - tw + kRound - 1) / kRound : 0;
-  struct Entry { uint32_t sub; float sk, lsv; };
-  auto entry_of = [&](int e, int i0) {
-    const int t = entry_token(i0);
-    e = min(max(e, 0), p.c.n_blocks - 1);
-    const Pair sc = p.c.scales[e];
-    return Entry{((uint32_t)e << (sh - 3)) + ((uint32_t)(t & (T - 1)) >> 4), key_scale(sc.x, sc.y),
-                     log_scale(sc.y)};
-  };
-  const uint32_t v_sub = (uint32_t)T >> 4;          // from a key subtile to its value subtile
-  auto load = [&](Tile<D>& x, const Entry& en, int i) {
-#pragma unroll
-    for (int a = 0; a < 2; ++a) {
-      const int l = 2 * (i & 31) + a;
-      const uint32_t sub = __builtin_amdgcn_readlane(en.sub, l);
-      x.sk[a] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(en.sk), l));
-      x.lsv[a] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(en.lsv), l));
-      const uint8_t* kb = p.c.codes + (uint64_t)sub * (16 * D) + lane * 16;
-      const uint8_t* vb = p.c.codes + (uint64_t)(sub + v_sub) * (16 * D) + lane * 16;
-#pragma unroll
-      for (int n = 0; n < N; ++n)
-        x.k[a][n] = load_codes<RG>(kb + n * 1024);
-#pragma unroll
-      for (int n = 0; n < N; ++n)
-        x.v[a][n] = load_codes<RG>(vb + n * 1024);
-    }
-  };
-  // A step's codes are loaded NB - 1 steps ahead, past the last one the last again; the entries of
-  // the next 32 steps while these 32 run.
-  Entry now, next;
-  Tile<D> x[NB];
-  auto fetch = [&](Tile<D>& y, int i) {
-    if (i > 0 && (i & 31) == 0) {
-      now = next;
-      next = entry_of(table[entry_token(i + 32) >> sh], i + 32);
-    }
-    load(y, now, min(i, steps - 1));
-  };
-  if (steps > 0) {
-    now = entry_of(entry0, 0);
-    next = entry_of(entry1, 32);
-#pragma unroll
-    for (int u = 0; u < NB - 1; ++u) fetch(x[u], u);
-  }
-
-  scale_queries<D, RT>(p, raw, q, qs);
-
-  State<D, RT> s;
-  reset(s);
-  const SubSums sums = {SUMS ? p.sub + head * p.sub_per_head * p.rows : nullptr, row0, p.rows};
-  // ---- finished blocks
-  auto compute = [&](const Tile<D>& y, int i) {
-    const int t = tw + i * kRound;
-    f4 sc[1][RT][2];
-    float fk[1][RT][2];
-#pragma unroll
-    for (int r = 0; r < RT; ++r) sc[0][r][0] = sc[0][r][1] = (f4){0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-    for (int n = 0; n < N; ++n)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        h8 k[2];
-#pragma unroll
-        for (int a = 0; a < 2; ++a) k[a] = code8<E4M3>(y.k[a][n][2 * h], y.k[a][n][2 * h + 1]);
-#pragma unroll
-        for (int r = 0; r < RT; ++r)
-#pragma unroll
-          for (int a = 0; a < 2; ++a) sc[0][r][a] = mfma_f16(k[a], q[r][2 * n + h], sc[0][r][a]);
-      }
+    // queries: row r of the tile in column `col`, channels i*64 + quad*16 + h*8 + e
+    h8 q[RT][2 * N];
+    float qs[RT];
+    int lim[RT];
+    int lm[RT];
+    int lim_lo = 0x7fffffff;
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
-      fk[0][r][0] = y.sk[0] * qs[r];
-      fk[0][r][1] = y.sk[1] * qs[r];
+      lm[r] = row_limit(p, it.b, it.ctx, row0 + r * 16 + col);
+      lim[r] = lm[r] < 0 ? 0x7fffffff : lm[r];       // rows without a query see everything
+      lim_lo = min(lim_lo, lim[r]);
     }
-    float d[2], pr[RT][8];
-    begin_steps<D, RT, 1>(s, sc, fk, lim, lim_lo, t, e8, y.lsv, quad, d);
-    finish_step<D, RT, SUMS ? kSubSums : kPlain>(s, sc[0], fk[0], d, t, e8, col, quad, sums, pr);
-    h8 ph[RT];
-    to_operand<RT>(pr, ph);
+    Raw raw[RT][2 * N];
+    load_queries<D, RT>(p, it.b, g, row0, col, quad, lm, raw);
 #pragma unroll
-    for (int n = 0; n < N; ++n)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const h8 v = code8<E4M3>(y.v[0][n][j], y.v[1][n][j]);
-#pragma unroll
-        for (int r = 0; r < RT; ++r) s.o[r][n * 4 + j] = mfma_f16(v, ph[r], s.o[r][n * 4 + j]);
-      }
-  };
-  if (steps > 0) {
-    for (int i = 0; i < steps; i += NB) {
-#pragma unroll
-      for (int u = 0; u < NB; ++u) {
-        fetch(x[(u + NB - 1) % NB], i + u + NB - 1);
-        if (i + u < steps) compute(x[u], i + u);
-      }
-    }
-  }
+    for (int o = 8; o >= 1; o >>= 1) lim_lo = min(lim_lo, __shfl_xor(lim_lo, o));
+    lim_lo = __builtin_amdgcn_readfirstlane(lim_lo);
 
-  if (full < it.t1)
-    unfinished_block<D, RT, SUMS>(p, s, it.b, g, it.ctx, it.ctx, full + 32 * token_wave, kRound, row0,
-                                  lim, lim_lo, sums, fresh(tid_lane));
+    const int steps = e8 > tw ? (e8 - tw + kRound - 1) / kRound : 0;
+    struct Entry { uint32_t sub; float sk, lsv; };
+    auto entry_of = [&](int e, int i0) {
+      const int t = entry_token(i0);
+      e = min(max(e, 0), p.c.n_blocks - 1);
+      const Pair sc = p.c.scales[e];
+      return Entry{((uint32_t)e << (sh - 3)) + ((uint32_t)(t & (T - 1)) >> 4), key_scale(sc.x, sc.y),
+                       log_scale(sc.y)};
+    };
+    const uint32_t v_sub = (uint32_t)T >> 4;          // from a key subtile to its value subtile
+    auto load = [&](Tile<D>& x, const Entry& en, int i) {
+#pragma unroll
+      for (int a = 0; a < 2; ++a) {
+        const int l = 2 * (i & 31) + a;
+        const uint32_t sub = __builtin_amdgcn_readlane(en.sub, l);
+        x.sk[a] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(en.sk), l));
+        x.lsv[a] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(en.lsv), l));
+        const uint8_t* kb = p.c.codes + (uint64_t)sub * (16 * D) + lane * 16;
+        const uint8_t* vb = p.c.codes + (uint64_t)(sub + v_sub) * (16 * D) + lane * 16;
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+          x.k[a][n] = load_codes<RG>(kb + n * 1024);
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+          x.v[a][n] = load_codes<RG>(vb + n * 1024);
+      }
+    };
+    // A step's codes are loaded NB - 1 steps ahead, past the last one the last again; the entries of
+    // the next 32 steps while these 32 run.
+    Entry now, next;
+    Tile<D> x[NB];
+    auto fetch = [&](Tile<D>& y, int i) {
+      if (i > 0 && (i & 31) == 0) {
+        now = next;
+        next = entry_of(table[entry_token(i + 32) >> sh], i + 32);
+      }
+      load(y, now, min(i, steps - 1));
+    };
+    if (steps > 0) {
+      now = entry_of(entry0, 0);
+      next = entry_of(entry1, 32);
+#pragma unroll
+      for (int u = 0; u < NB - 1; ++u) fetch(x[u], u);
+    }
 
-  lane = fresh(tid_lane);
-  col = lane & 15;
-  quad = lane >> 4;
-  // ---- the token waves' states merged, normalized and written as the part's partial
+    scale_queries<D, RT>(p, raw, q, qs);
+
+    State<D, RT> s;
+    reset(s);
+    const SubSums sums = {SUMS ? p.sub + head * p.sub_per_head * p.rows : nullptr, row0, p.rows};
+    // ---- finished blocks
+    auto compute = [&](const Tile<D>& y, int i) {
+      const int t = tw + i * kRound;
+      f4 sc[1][RT][2];
+      float fk[1][RT][2];
 #pragma unroll
-  for (int r = 0; r < RT; ++r) {
-    const float l = quad_sum(s.l[r]);
-    if (quad == 0) {
-      sm[wave][r * 16 + col] = s.m[r];
-      sl[wave][r * 16 + col] = l;
+      for (int r = 0; r < RT; ++r) sc[0][r][0] = sc[0][r][1] = (f4){0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          h8 k[2];
+#pragma unroll
+          for (int a = 0; a < 2; ++a) k[a] = code8<E4M3>(y.k[a][n][2 * h], y.k[a][n][2 * h + 1]);
+#pragma unroll
+          for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int a = 0; a < 2; ++a) sc[0][r][a] = mfma_f16(k[a], q[r][2 * n + h], sc[0][r][a]);
+        }
+#pragma unroll
+      for (int r = 0; r < RT; ++r) {
+        fk[0][r][0] = y.sk[0] * qs[r];
+        fk[0][r][1] = y.sk[1] * qs[r];
+      }
+      float d[2], pr[RT][8];
+      begin_steps<D, RT, 1>(s, sc, fk, lim, lim_lo, t, e8, y.lsv, quad, d);
+      finish_step<D, RT, SUMS ? kSubSums : kPlain>(s, sc[0], fk[0], d, t, e8, col, quad, sums, pr);
+      h8 ph[RT];
+      to_operand<RT>(pr, ph);
+#pragma unroll
+      for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const h8 v = code8<E4M3>(y.v[0][n][j], y.v[1][n][j]);
+#pragma unroll
+          for (int r = 0; r < RT; ++r) s.o[r][n * 4 + j] = mfma_f16(v, ph[r], s.o[r][n * 4 + j]);
+        }
+    };
+    if (steps > 0) {
+      for (int i = 0; i < steps; i += NB) {
+#pragma unroll
+        for (int u = 0; u < NB; ++u) {
+          fetch(x[(u + NB - 1) % NB], i + u + NB - 1);
+          if (i + u < steps) compute(x[u], i + u);
+        }
+      }
     }
-  }
-  __syncthreads();
-  const int64_t slot0 = ((int64_t)(blockIdx.x + it.b) * p.c.n_kv + g) * p.rows;
-  const float vref = exp2_fast(s.lv);
+
+    if (full < it.t1)
+      unfinished_block<D, RT, SUMS>(p, s, it.b, g, it.ctx, it.ctx, full + 32 * token_wave, kRound, row0,
+                                    lim, lim_lo, sums, fresh(tid_lane));
+
+    lane = fresh(tid_lane);
+    col = lane & 15;
+    quad = lane >> 4;
+    // ---- the token waves' states merged, normalized and written as the part's partial
 #pragma unroll
-  for (int r = 0; r < RT; ++r) {
-    const int group = wave % RG;
-    float M = -__builtin_inff();
-#pragma unroll
-    for (int w = 0; w < TW; ++w) M = fmaxf(M, sm[w * RG + group][r * 16 + col]);
-    float L = 0.0f, own = 0.0f;
-#pragma unroll
-    for (int w = 0; w < TW; ++w) {
-      const float mw = sm[w * RG + group][r * 16 + col], lw = sl[w * RG + group][r * 16 + col];
-      const float a = mw == M ? 1.0f : exp2_fast(mw - M);
-      // a wave without tokens: sum 0 (NaN stays)
-      L += lw * a;
-      if (w == token_wave) own = a;
-    }
-    const float f = L == 0.0f ? 0.0f : own / L;
-    if (token_wave == 0 && quad == 0 && row0 + r * 16 + col < p.rows)
-      p.part_ml[slot0 + row0 + r * 16 + col] = {M, L};
-#pragma unroll
-    for (int c = 0; c < CT; ++c) {
-      f4 v = s.o[r][c] * f;                         // at most the largest code, then the scale
-      v *= vref;
-      *reinterpret_cast<f4*>(&so[wave][col][c * 16 + quad * 4]) = v;
+    for (int r = 0; r < RT; ++r) {
+      const float l = quad_sum(s.l[r]);
+      if (quad == 0) {
+        sm[wave][r * 16 + col] = s.m[r];
+        sl[wave][r * 16 + col] = l;
+      }
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < RG * 16 * D / 4; i += 256) {
-      const int gr = i / (16 * D / 4), row = i / (D / 4) % 16, ch = i % (D / 4) * 4;
-      const int to = gr * (16 * RT) + r * 16 + row;
-      if (to < p.rows) {
-        f4 v = *reinterpret_cast<const f4*>(&so[gr][row][ch]);
+    const int64_t slot0 = ((int64_t)(blockIdx.x + it.b) * p.c.n_kv + g) * p.rows;
+    const float vref = exp2_fast(s.lv);
 #pragma unroll
-        for (int w = 1; w < TW; ++w) v += *reinterpret_cast<const f4*>(&so[w * RG + gr][row][ch]);
-        *reinterpret_cast<f4*>(p.part_o + (slot0 + to) * D + ch) = v;
+    for (int r = 0; r < RT; ++r) {
+      const int group = wave % RG;
+      float M = -__builtin_inff();
+#pragma unroll
+      for (int w = 0; w < TW; ++w) M = fmaxf(M, sm[w * RG + group][r * 16 + col]);
+      float L = 0.0f, own = 0.0f;
+#pragma unroll
+      for (int w = 0; w < TW; ++w) {
+        const float mw = sm[w * RG + group][r * 16 + col], lw = sl[w * RG + group][r * 16 + col];
+        const float a = mw == M ? 1.0f : exp2_fast(mw - M);
+        // a wave without tokens: sum 0 (NaN stays)
+        L += lw * a;
+        if (w == token_wave) own = a;
       }
+      const float f = L == 0.0f ? 0.0f : own / L;
+      if (token_wave == 0 && quad == 0 && row0 + r * 16 + col < p.rows)
+        p.part_ml[slot0 + row0 + r * 16 + col] = {M, L};
+#pragma unroll
+      for (int c = 0; c < CT; ++c) {
+        f4 v = s.o[r][c] * f;                         // at most the largest code, then the scale
+        v *= vref;
+        *reinterpret_cast<f4*>(&so[wave][col][c * 16 + quad * 4]) = v;
+      }
+      __syncthreads();
+      for (int i = threadIdx.x; i < RG * 16 * D / 4; i += 256) {
+        const int gr = i / (16 * D / 4), row = i / (D / 4) % 16, ch = i % (D / 4) * 4;
+        const int to = gr * (16 * RT) + r * 16 + row;
+        if (to < p.rows) {
+          f4 v = *reinterpret_cast<const f4*>(&so[gr][row][ch]);
+#pragma unroll
+          for (int w = 1; w < TW; ++w) v += *reinterpret_cast<const f4*>(&so[w * RG + gr][row][ch]);
+          *reinterpret_cast<f4*>(p.part_o + (slot0 + to) * D + ch) = v;
+        }
+      }
+      __syncthreads();
     }
-    __syncthreads();
-  }
-  at = pl.start + units_of(pl.ctx);
-  if (at >= at_end || !find_unit(p, lens, at, tid_lane, &pl)) return;
+    at = pl.start + units_of(pl.ctx);
+    if (at >= at_end || !find_unit(p, lens, at, tid_lane, &pl)) return;
   }
 }
 
