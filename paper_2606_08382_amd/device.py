@@ -182,7 +182,7 @@ def _array(name, t, shape, dtype, device):
 
 def _vector(name, t, shape, dtype, device):
     """Checks a packed array of int32 (dtype "int32") or float32."""
-    if str(t.dtype) != "torch." + dtype:
+    if str(t.dtype)[6:] != dtype:
         raise TypeError(f"{name}: {t.dtype}, expected {dtype}")
     if t.device != device:
         raise ValueError(f"{name} is on {t.device}, the layer on {device}")
@@ -190,29 +190,17 @@ def _vector(name, t, shape, dtype, device):
         raise ValueError(f"{name}: expected a contiguous array of shape {tuple(shape)}")
 
 
-class _On:
-    """Makes the arrays' device current for a call; yields the given stream, or torch's current
-    one on that device (its handle alone: the stream object would cost 2 us a call)."""
-
-    __slots__ = ("stream", "other")
-
-    def __init__(self, device, stream):
-        import torch
-        if stream is None:
-            stream = torch._C._cuda_getCurrentRawStream(device.index)
-        self.stream = stream
-        self.other = None
-        if torch.cuda.current_device() != device.index:
-            self.other = torch.cuda.device(device)
-
-    def __enter__(self):
-        if self.other is not None:
-            self.other.__enter__()
-        return self.stream
-
-    def __exit__(self, *exc):
-        if self.other is not None:
-            self.other.__exit__(*exc)
+def _run(device, stream, fn, *args):
+    """fn(*args, stream=...) with the arrays' device current; on torch's current stream there unless
+    one is given (its handle alone: the stream object would cost 2 us a call)."""
+    import torch
+    if stream is None:
+        stream = torch._C._cuda_getCurrentRawStream(device.index)
+    if torch.cuda.current_device() == device.index:
+        fn(*args, stream=stream)
+    else:
+        with torch.cuda.device(device):
+            fn(*args, stream=stream)
 
 
 def _cuda(device):
@@ -250,9 +238,8 @@ class Rope:
         _vector("positions", pos, shape[:2], "int32", x.device)
         if 0 in shape:
             return out
-        with _On(x.device, stream) as stream:
-            S.starkv_rope(self.plan, a, xs, o, os_, pos, shape[0], shape[1], shape[2],
-                          int(inverse), stream=stream)
+        _run(x.device, stream, S.starkv_rope, self.plan, a, xs, o, os_, pos, shape[0], shape[1],
+             shape[2], int(inverse))
         return out
 
 
@@ -309,9 +296,8 @@ class DenseLayer:
             self._lengths("n_new", n_new)
         if shape[1] == 0:
             return
-        with _On(self.device, stream) as stream:
-            S.starkv_dense_append(self.plan, self.cache, k, ks, v, vs, pos, shape[1], n_new,
-                                  stream=stream)
+        _run(self.device, stream, S.starkv_dense_append, self.plan, self.cache, k, ks, v, vs, pos,
+             shape[1], n_new)
 
     def read(self, ctx_len, start, k_out, v_out, stream=None):
         """Rows start[b] .. of the cache into k_out, v_out [B][n][H_kv][d] (16 or 32 bits)."""
@@ -327,9 +313,8 @@ class DenseLayer:
         self._lengths("start", start)
         if shape[1] == 0:
             return
-        with _On(self.device, stream) as stream:
-            S.starkv_dense_read(self.plan, self.cache, ctx_len, start, shape[1], k_out, ks, v_out,
-                                vs, dtype, stream=stream)
+        _run(self.device, stream, S.starkv_dense_read, self.plan, self.cache, ctx_len, start,
+             shape[1], k_out, ks, v_out, vs, dtype)
 
     def workspace(self, n_q=1, weights=False):
         """The workspace that ``attend`` uses for n_q query tokens.  It is kept, so a captured
@@ -363,10 +348,8 @@ class DenseLayer:
             return out
         if ws is None:
             ws = self.workspace(shape[1], weights is not None)
-        with _On(self.device, stream) as stream:
-            S.starkv_dense_attn(self.plan, self.cache, a, qs, shape[1], q_len, ctx_len,
-                                self.capacity if max_ctx is None else max_ctx, o, os_, weights,
-                                ws, stream=stream)
+        _run(self.device, stream, S.starkv_dense_attn, self.plan, self.cache, a, qs, shape[1],
+             q_len, ctx_len, self.capacity if max_ctx is None else max_ctx, o, os_, weights, ws)
         return out
 
     def evict(self, weights, ctx_len, keep, sink=0, recent=0, table_out=None, weights_out=None,
@@ -383,9 +366,8 @@ class DenseLayer:
             _vector("weights_out", weights_out, shape, "float32", self.device)
         if ctx_out is not None:
             self._lengths("ctx_out", ctx_out)
-        with _On(self.device, stream) as stream:
-            S.starkv_dense_evict(self.plan, weights, ctx_len, keep, sink, recent, table_out,
-                                 weights_out, ctx_out, stream=stream)
+        _run(self.device, stream, S.starkv_dense_evict, self.plan, weights, ctx_len, keep, sink,
+             recent, table_out, weights_out, ctx_out)
         return (self.table if table_out is None else table_out,
                 weights if weights_out is None else weights_out,
                 ctx_len if ctx_out is None else ctx_out)
