@@ -108,7 +108,8 @@ __device__ __forceinline__ float from16(uint32_t u, int bf16) {
 
 // ---- work plan ----------------------------------------------------------------------
 // The sequences' tokens, in units of kUnit, lie end to end; range w of p.ranges takes the units
-// [w R, (w + 1) R), R = ceil(all units / ranges), and with them the end of one sequence and the
+// [w R, (w + 1) R), R = ceil(all units / ranges) (at least p.min_units where that leaves none idle),
+// and with them the end of one sequence and the
 // start of the next: ranges are equal however ragged the lengths are.  The part of sequence b in
 // range w is slot w + b of the partials (one of the two grows from part to part), at most
 // ranges + B of them.  Every wave derives this from the lengths, so nothing is planned on the
@@ -145,7 +146,8 @@ __device__ __forceinline__ int range_units(const DenseAttnParams& p, const Lens&
     const int b = b0 + lane;
     sum += __builtin_amdgcn_readlane(wave_scan(b < p.c.batch ? units_of(clamp_ctx(p, b)) : 0), 63);
   }
-  return max((int)(((uint32_t)sum + (uint32_t)p.ranges - 1) / (uint32_t)p.ranges), p.min_units);
+  const int R = max((int)(((uint32_t)sum + (uint32_t)p.ranges - 1) / (uint32_t)p.ranges), 1);
+  return sum >= p.ranges ? max(R, p.min_units) : R;
 }
 
 // The sequence that holds unit `at`, its length and its first unit; false past the last.

@@ -486,7 +486,7 @@ starkv_status starkv_dense_attn(const starkv_dense_plan* P, const void* cache, c
   p.max_ctx = max_ctx;
   p.ranges = (int32_t)w.ranges;
   // (a chunk workgroup's start and end cost more than a tile: 100 queries over 2000 tokens 32 us
-  // against 38 with one unit)
+  // against 38 with one unit; not where there are fewer units than ranges)
   p.min_units = p.rows > kSplitRows ? 2 : 1;
   p.sub_per_head = w.sub_per_head;
   p.q_wide = rows_wide(q, a, 2);
